@@ -15,9 +15,9 @@ SRC_DIR = os.path.join(PKG, "csrc")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfpdt.so")
 SOURCES = ["api.hip", "pack.hip", "fwd_bf16.hip", "bwd_bf16.hip", "f32_path.hip", "calibrate.hip"]
-# token-wise chunked neighbours (projection, feed-forward block, loss): a library of their own
+# token-wise neighbours (projection, feed-forward block, loss; rotary positions, normalisation, optimizer): a library of their own
 TW_LIB = os.path.join(PKG, "libfpdt_tokenwise.so")
-TW_SOURCES = ["tokenwise.hip", "tw_gemm.hip"]
+TW_SOURCES = ["tokenwise.hip", "tw_gemm.hip", "tw_rope.hip", "tw_norm.hip", "tw_optim.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -packed-fp32-ops off: packed fp32 VALU forms are kept out of the generated code.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -10,14 +10,15 @@
 #include <string>
 
 #include "../../include/fpdt_tokenwise.h"
+#include "tw_common.h"
 #include "tw_gemm.h"
 #include "tw_plan.h"
 
-namespace {
-
-enum { TW_OK = 0, TW_INVALID = 1, TW_UNSUPPORTED = 2, TW_WORKSPACE = 3, TW_HIP = 4 };
+namespace fpdt_tw {
 
 thread_local std::string g_err;
+
+void clear_error() { g_err.clear(); }
 
 int fail(int code, const char* fmt, ...)
 {
@@ -26,15 +27,20 @@ int fail(int code, const char* fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    g_err = buf;
+    try {
+        g_err = buf;
+    } catch (...) {  // no memory for the text: the code alone
+        g_err.clear();
+    }
     return code;
 }
 
-#define HIP_TRY(expr)                                                                            \
-    do {                                                                                         \
-        hipError_t e_ = (expr);                                                                  \
-        if (e_ != hipSuccess) return fail(TW_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
+}  // namespace fpdt_tw
+
+namespace {
+
+using namespace fpdt_tw;
+
 std::mutex g_mu;
 
 // The dense products are this library's own MFMA kernels (tw_gemm.hip).  A "handle" is just the

@@ -1,0 +1,83 @@
+// What the sources of the token-wise library share: status codes and the error text (tokenwise.hip), accesses of
+// several elements, conversions, sums over lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fpdt_tw {
+
+enum { TW_OK = 0, TW_INVALID = 1, TW_UNSUPPORTED = 2, TW_WORKSPACE = 3, TW_HIP = 4 };
+
+// Sets the calling thread's error text and returns `code`.
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+void clear_error();
+
+#define HIP_TRY(expr)                                                                            \
+    do {                                                                                         \
+        hipError_t e_ = (expr);                                                                  \
+        if (e_ != hipSuccess) return fail(TW_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
+    } while (0)
+
+// Do the byte ranges [a, a + na) and [b, b + nb) meet?
+inline bool ranges_meet(const void* a, size_t na, const void* b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na && nb && x < y + nb && y < x + na;
+}
+
+inline bool misaligned(const void* p, size_t by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }
+
+// V elements in one access.  The address need only be aligned to an element: global memory is read and written at
+// any address here, at the price of the cache lines that an access touches.
+template <class T, int V> struct Vec {
+    T e[V];
+};
+template <int V, class T> __device__ __forceinline__ Vec<T, V> load(const T* p)
+{
+    Vec<T, V> v;
+    __builtin_memcpy(&v, p, sizeof v);
+    return v;
+}
+template <int V, class T> __device__ __forceinline__ void store(T* p, const Vec<T, V>& v) { __builtin_memcpy(p, &v, sizeof v); }
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((unsigned)x << 16); }
+// rounded to the type, to nearest even
+template <class T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t from_float<uint16_t>(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+template <int V> __device__ __forceinline__ Vec<float, V> rounded(const float* x, float)
+{
+    Vec<float, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v.e[i] = x[i];
+    return v;
+}
+template <int V> __device__ __forceinline__ Vec<uint16_t, V> rounded(const float* x, uint16_t)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    Vec<uint16_t, V> v;
+    if constexpr (V == 1) {
+        v.e[0] = from_float<uint16_t>(x[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            const unsigned two = __builtin_bit_cast(unsigned, __builtin_convertvector((floatx2{x[i], x[i + 1]}), bf16x2));
+            v.e[i] = (uint16_t)two;
+            v.e[i + 1] = (uint16_t)(two >> 16);
+        }
+    }
+    return v;
+}
+
+// Sum over `lanes` consecutive lanes (a power of two), in every one of them.
+template <int LANES, class F> __device__ __forceinline__ F lanes_sum(F v)
+{
+#pragma unroll
+    for (int m = LANES / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+    return v;
+}
+
+}  // namespace fpdt_tw

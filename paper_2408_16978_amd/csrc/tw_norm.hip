@@ -1,0 +1,439 @@
+// Normalisation of rows with the residual add in front of it (include/fpdt_tokenwise.h: fpdt_tw_norm_*).
+//
+//     s = x + r,   u = (s - mean) rstd,   y = u w + b          (RMS: mean = 0, b = 0)
+//     h = dy w,    dx = rstd (h - mean(h) - u mean(h u)) + dr  (RMS: without mean(h))
+//     dw += sum_rows dy u,   db += sum_rows dy
+//
+// Bound by the memory: a row stays in the registers of the lanes that read it, so each tensor is read or written once.
+#include <cmath>
+
+#include "../../include/fpdt_tokenwise.h"
+#include "tw_common.h"
+
+namespace {
+
+using namespace fpdt_tw;
+
+constexpr int MOST_HIDDEN = 16384;
+
+// Sums of N values over the LANES threads (at most a wave: lanes of it; more: whole waves of the workgroup) of a row,
+// in every one of them.  `red` holds two sums of 16 waves, by turns, so that one barrier is enough.
+template <int LANES, int N> struct RowSum {
+    float (*red)[N][16];
+    int turn = 0;
+    __device__ void operator()(float (&v)[N])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[n]);
+        if constexpr (LANES > 64) {
+            constexpr int W = LANES / 64;
+            const int w = threadIdx.x / 64;
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int n = 0; n < N; ++n) red[turn][n][w] = v[n];
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                v[n] = 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[n] += red[turn][n][i];
+            }
+            turn ^= 1;
+        }
+    }
+};
+
+// Access i of a lane covers columns [c, c + V), c = (i LANES + lane) V; the last one of a row may be cut off.
+template <class T, int V> __device__ __forceinline__ Vec<T, V> load_cut(const T* p, int c, int hidden)
+{
+    if (c + V <= hidden) return load<V>(p + c);
+    Vec<T, V> v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.e[e] = c + e < hidden ? p[c + e] : T(0);
+    return v;
+}
+template <class T, int V> __device__ __forceinline__ void store_cut(T* p, int c, int hidden, const Vec<T, V>& v)
+{
+    if (c + V <= hidden) {
+        store(p + c, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (c + e < hidden) p[c + e] = v.e[e];
+}
+
+// Rows of LANES threads, NA accesses of V elements each; max(LANES, 256) threads.
+template <class T, int LANES, int NA, bool LAYER>
+__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats,
+                                                                               int64_t rows, int hidden, float eps)
+{
+    constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES;
+    __shared__ float red[2][1][16];
+    RowSum<LANES, 1> sum{red};
+    const int lane = threadIdx.x % LANES;
+    const float inv = 1.f / hidden;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
+        if (row >= rows) break;  // (only where rows are lanes of a wave: no barrier is left out)
+        Vec<T, V> x[NA], r[NA];
+        float s[NA][V];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+            if (c < hidden) x[i] = load_cut<T, V>(X + at, c, hidden);
+        }
+        if (R)
+#pragma unroll
+            for (int i = 0; i < NA; ++i) {
+                const int c = (i * LANES + lane) * V;
+                if (c < hidden) r[i] = load_cut<T, V>(R + at, c, hidden);
+            }
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+            if (c < hidden) {
+                if (R) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s[i][e] = to_float(x[i].e[e]) + to_float(r[i].e[e]);
+                    x[i] = rounded<V>(s[i], T());  // what the backward reads is what is normalised
+                    if (S) store_cut<T, V>(S + at, c, hidden, x[i]);
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[i][e] = to_float(x[i].e[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[i][e] = 0.f;
+            }
+        }
+        float mean = 0.f;
+        if (LAYER) {
+            float v[1] = {0.f};
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[0] += s[i][e];
+            sum(v);
+            mean = v[0] * inv;
+        }
+        float v[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (LAYER) s[i][e] = c + e < hidden ? s[i][e] - mean : 0.f;
+                v[0] = fmaf(s[i][e], s[i][e], v[0]);
+            }
+        }
+        sum(v);
+        const float rstd = 1.f / sqrtf(v[0] * inv + eps);
+        if (stats && lane == 0) {
+            if (LAYER) stats[row] = mean;
+            stats[(LAYER ? rows : 0) + row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+            if (c >= hidden) continue;
+            const Vec<T, V> w = load_cut<T, V>(W, c, hidden);
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[i][e] *= rstd * to_float(w.e[e]);
+            if (LAYER && B) {
+                const Vec<T, V> b = load_cut<T, V>(B, c, hidden);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[i][e] += to_float(b.e[e]);
+            }
+            store_cut<T, V>(Y + at, c, hidden, rounded<V>(s[i], T()));
+        }
+    }
+}
+
+// Groups of LANES threads walk the rows; a thread keeps its columns' shares of dw and db in registers, a workgroup's
+// groups add theirs up in LDS and leave one row of partial sums each for norm_sums_kernel: no atomics, the same order
+// of sums in every call.
+template <class T, int LANES, int NA, bool LAYER>
+__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
+                                                                               float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
+{
+    constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES, N = LAYER ? 2 : 1;
+    __shared__ float red[2][N][16];
+    RowSum<LANES, N> sum{red};
+    const int lane = threadIdx.x % LANES;
+    const float inv = 1.f / hidden;
+    float w[NA][V], dw[NA][V], db[NA][V];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        const int c = (i * LANES + lane) * V;
+        Vec<T, V> x;
+        if (c < hidden) x = load_cut<T, V>(W, c, hidden);
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[i][e] = c < hidden ? to_float(x.e[e]) : 0.f, dw[i][e] = db[i][e] = 0.f;
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
+        if (row >= rows) break;
+        Vec<T, V> x[NA], y[NA], r[NA];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+            if (c < hidden) x[i] = load_cut<T, V>(S + at, c, hidden), y[i] = load_cut<T, V>(dY + at, c, hidden);
+        }
+        if (dR)
+#pragma unroll
+            for (int i = 0; i < NA; ++i) {
+                const int c = (i * LANES + lane) * V;
+                if (c < hidden) r[i] = load_cut<T, V>(dR + at, c, hidden);
+            }
+        const float mean = LAYER ? stats[row] : 0.f, rstd = stats[(LAYER ? rows : 0) + row];
+        float v[N] = {};
+        float u[NA][V], h[NA][V];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool in = c + e < hidden;
+                const float dy = in ? to_float(y[i].e[e]) : 0.f;
+                u[i][e] = in ? (to_float(x[i].e[e]) - mean) * rstd : 0.f;
+                h[i][e] = dy * w[i][e];
+                v[0] = fmaf(h[i][e], u[i][e], v[0]);
+                if (LAYER) v[N - 1] += h[i][e], db[i][e] += dy;
+                dw[i][e] = fmaf(dy, u[i][e], dw[i][e]);
+            }
+        }
+        sum(v);
+        const float along = v[0] * inv, level = LAYER ? v[N - 1] * inv : 0.f;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int c = (i * LANES + lane) * V;
+            if (c >= hidden) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                h[i][e] = rstd * (h[i][e] - level - u[i][e] * along);
+                if (dR) h[i][e] += to_float(r[i].e[e]);
+            }
+            store_cut<T, V>(dX + at, c, hidden, rounded<V>(h[i], T()));
+        }
+    }
+    if (!want_w && !want_b) return;
+    __shared__ float lds[ROWS > 1 ? ROWS : 1][ROWS > 1 ? NA * V * LANES : 1];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (k == 0 ? !want_w : !want_b) continue;
+        float* out = partial + ((int64_t)(k == 1 && want_w ? gridDim.x : 0) + blockIdx.x) * hidden;
+        float(&d)[NA][V] = k == 0 ? dw : db;
+        if constexpr (ROWS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) lds[threadIdx.x / LANES][(i * LANES + lane) * V + e] = d[i][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < hidden; c += THREADS) {
+                float v = 0.f;
+#pragma unroll
+                for (int g = 0; g < ROWS; ++g) v += lds[g][c];
+                out[c] = v;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int c = (i * LANES + lane) * V + e;
+                    if (c < hidden) out[c] = d[i][e];
+                }
+        }
+    }
+}
+
+// dw[c] += sum over the n rows of partial sums, (db: the same, behind them).  64 columns and 16 waves a workgroup.
+__global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, int n, int hidden, float* d0, float* d1)
+{
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x % 64, w = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const float* p = partial + (int64_t)blockIdx.y * n * hidden + c;
+    float v = 0.f;
+    if (c < hidden)
+        for (int r = w; r < n; r += 16) v += p[(int64_t)r * hidden];
+    part[w][lane] = v;
+    __syncthreads();
+    if (w || c >= hidden) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += part[i][lane];
+    float* d = blockIdx.y == 0 ? d0 : d1;
+    d[c] += v;
+}
+
+// Rows of partial sums (workgroups of the backward) at most.
+constexpr int BWD_GROUPS = 1024;
+
+// f(lanes, accesses) as integral constants for a row of n accesses
+template <int L, int N> struct Shape {
+    static constexpr int lanes = L, accesses = N;
+};
+template <class F> void fwd_shape(int n, F f)
+{
+    if (n <= 16) f(Shape<16, 1>());
+    else if (n <= 32) f(Shape<16, 2>());
+    else if (n <= 64) f(Shape<64, 1>());
+    else if (n <= 128) f(Shape<64, 2>());
+    else if (n <= 256) f(Shape<64, 4>());
+    else if (n <= 512) f(Shape<64, 8>());
+    else if (n <= 1024) f(Shape<256, 4>());
+    else if (n <= 2048) f(Shape<256, 8>());
+    else f(Shape<1024, 4>());
+}
+template <class F> void bwd_shape(int n, F f)
+{
+    if (n <= 16) f(Shape<16, 1>());
+    else if (n <= 64) f(Shape<64, 1>());
+    else if (n <= 128) f(Shape<64, 2>());
+    else if (n <= 256) f(Shape<256, 1>());
+    else if (n <= 512) f(Shape<256, 2>());
+    else if (n <= 1024) f(Shape<256, 4>());
+    else if (n <= 2048) f(Shape<1024, 2>());
+    else f(Shape<1024, 4>());
+}
+
+int check(int64_t rows, int hidden, int kind, int dtype)
+{
+    if (rows <= 0 || hidden <= 0) return fail(TW_INVALID, "rows and hidden must be positive");
+    if (kind != FPDT_TW_RMSNORM && kind != FPDT_TW_LAYERNORM) return fail(TW_INVALID, "unknown kind %d", kind);
+    if (dtype != FPDT_TW_F32 && dtype != FPDT_TW_BF16) return fail(TW_INVALID, "unknown dtype %d", dtype);
+    if (hidden > MOST_HIDDEN || rows > INT32_MAX) return fail(TW_UNSUPPORTED, "hidden=%d beyond %d, or rows beyond the launch limits", hidden, MOST_HIDDEN);
+    return TW_OK;
+}
+
+// An output may be an input's own memory (each element is read before it is written, by the same thread), not part of it.
+int check_apart(const void* out, const char* name, const void* const* in, int n, size_t bytes)
+{
+    for (int i = 0; i < n; ++i)
+        if (out && in[i] && out != in[i] && ranges_meet(out, bytes, in[i], bytes)) return fail(TW_INVALID, "%s overlaps another tensor without being it", name);
+    return TW_OK;
+}
+
+unsigned groups_of(int64_t rows, int rows_at_once, int most)
+{
+    const int64_t n = (rows + rows_at_once - 1) / rows_at_once;
+    return (unsigned)(n < most ? n : most);
+}
+
+template <class T>
+void launch_fwd(const void* X, const void* R, const void* W, const void* B, void* S, void* Y, float* stats, int64_t rows, int hidden, int kind, float eps,
+                hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    auto t = [](const void* p) { return static_cast<const T*>(p); };
+    fwd_shape((hidden + V - 1) / V, [&](auto shape) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
+        const unsigned grid = groups_of(rows, THREADS / L, 1 << 22);
+        if (kind == FPDT_TW_LAYERNORM)
+            norm_fwd_kernel<T, L, N, true><<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+        else
+            norm_fwd_kernel<T, L, N, false><<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), nullptr, static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+    });
+}
+
+template <class T>
+void launch_bwd(const void* S, const void* W, const float* stats, const void* dY, const void* dR, void* dX, float* dW, float* dB, int64_t rows, int hidden,
+                int kind, float* partial, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    auto t = [](const void* p) { return static_cast<const T*>(p); };
+    bwd_shape((hidden + V - 1) / V, [&](auto shape) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
+        const unsigned grid = groups_of(rows, THREADS / L, BWD_GROUPS);
+        if (kind == FPDT_TW_LAYERNORM)
+            norm_bwd_kernel<T, L, N, true><<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
+        else
+            norm_bwd_kernel<T, L, N, false><<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, false);
+        if (dW || dB)
+            norm_sums_kernel<<<dim3((hidden + 63) / 64, dW && dB ? 2 : 1), 1024, 0, st>>>(partial, (int)grid, hidden, dW ? dW : dB, dB);
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int fpdt_tw_norm_fwd(const void* X, const void* R, const void* W, const void* B, void* S, void* Y, float* stats, int64_t rows, int hidden, int kind,
+                     float eps, int dtype, void* stream)
+{
+    clear_error();
+    if (!X || !W || !Y) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check(rows, hidden, kind, dtype);
+    if (rc != TW_OK) return rc;
+    if (S && !R) return fail(TW_INVALID, "S is the sum of X and R: R is NULL");
+    if (B && kind == FPDT_TW_RMSNORM) return fail(TW_INVALID, "RMSNORM has no bias");
+    if (!std::isfinite(eps) || eps < 0) return fail(TW_INVALID, "eps must be finite and not negative");
+    const size_t size = dtype == FPDT_TW_F32 ? 4 : 2, bytes = (size_t)rows * hidden * size;
+    const void* every[6] = {X, R, W, B, S, Y};
+    for (const void* p : every)
+        if (misaligned(p, size)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (misaligned(stats, 4)) return fail(TW_INVALID, "stats is not aligned to its elements");
+    const void* in[2] = {X, R};
+    if ((rc = check_apart(S, "S", in, 2, bytes)) != TW_OK || (rc = check_apart(Y, "Y", in, 2, bytes)) != TW_OK) return rc;
+    if (S && ranges_meet(S, bytes, Y, bytes)) return fail(TW_INVALID, "S and Y overlap");
+    const void* row[2] = {W, B};
+    const size_t nstats = (size_t)rows * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
+    for (const void* p : row)
+        if (p && (ranges_meet(S, S ? bytes : 0, p, hidden * size) || ranges_meet(Y, bytes, p, hidden * size))) return fail(TW_INVALID, "an output overlaps W or B");
+    for (const void* p : every)
+        if (stats && p && ranges_meet(stats, nstats, p, p == W || p == B ? hidden * size : bytes)) return fail(TW_INVALID, "stats overlaps a tensor");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (size == 4) launch_fwd<float>(X, R, W, B, S, Y, stats, rows, hidden, kind, eps, st);
+    else launch_fwd<uint16_t>(X, R, W, B, S, Y, stats, rows, hidden, kind, eps, st);
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+size_t fpdt_tw_norm_bwd_workspace_bytes(int64_t rows, int hidden, int kind)
+{
+    if (rows <= 0 || hidden <= 0 || hidden > MOST_HIDDEN || rows > INT32_MAX || (kind != FPDT_TW_RMSNORM && kind != FPDT_TW_LAYERNORM)) return 0;
+    // one row of partial sums per workgroup, and never more workgroups than rows
+    return (size_t)groups_of(rows, 1, BWD_GROUPS) * hidden * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
+}
+
+int fpdt_tw_norm_bwd(const void* S, const void* W, const float* stats, const void* dY, const void* dR, void* dX, float* dW, float* dB, int64_t rows,
+                     int hidden, int kind, int dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    clear_error();
+    if (!S || !W || !stats || !dY || !dX) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check(rows, hidden, kind, dtype);
+    if (rc != TW_OK) return rc;
+    if (dB && kind == FPDT_TW_RMSNORM) return fail(TW_INVALID, "RMSNORM has no bias");
+    const size_t size = dtype == FPDT_TW_F32 ? 4 : 2, bytes = (size_t)rows * hidden * size;
+    const void* every[5] = {S, W, dY, dR, dX};
+    for (const void* p : every)
+        if (misaligned(p, size)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (misaligned(stats, 4) || misaligned(dW, 4) || misaligned(dB, 4)) return fail(TW_INVALID, "stats, dW or dB is not aligned to its elements");
+    const size_t need = dW || dB ? fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind) : 0;
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 256)))
+        return fail(TW_WORKSPACE, "workspace NULL, misaligned or too small (%zu < %zu bytes)", workspace_bytes, need);
+    const void* in[3] = {S, dY, dR};
+    if ((rc = check_apart(dX, "dX", in, 3, bytes)) != TW_OK) return rc;
+    const size_t nstats = (size_t)rows * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1), ncol = (size_t)hidden * 4;
+    if (ranges_meet(dX, bytes, W, hidden * size) || ranges_meet(dX, bytes, stats, nstats)) return fail(TW_INVALID, "dX overlaps W or stats");
+    if (dW && dB && ranges_meet(dW, ncol, dB, ncol)) return fail(TW_INVALID, "dW and dB overlap");
+    // what is written besides dX meets nothing that is read, or dX
+    struct Out {
+        const void* p;
+        size_t n;
+    } outs[3] = {{dW, dW ? ncol : 0}, {dB, dB ? ncol : 0}, {workspace, need}};
+    for (const Out& o : outs) {
+        for (const void* p : every)
+            if (p && ranges_meet(o.p, o.n, p, p == W ? hidden * size : bytes)) return fail(TW_INVALID, "dW, dB or the workspace overlaps a tensor");
+        if (ranges_meet(o.p, o.n, stats, nstats)) return fail(TW_INVALID, "dW, dB or the workspace overlaps stats");
+    }
+    if (ranges_meet(workspace, need, dW, dW ? ncol : 0) || ranges_meet(workspace, need, dB, dB ? ncol : 0)) return fail(TW_INVALID, "the workspace overlaps dW or dB");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    float* partial = static_cast<float*>(workspace);
+    if (size == 4) launch_bwd<float>(S, W, stats, dY, dR, dX, dW, dB, rows, hidden, kind, partial, st);
+    else launch_bwd<uint16_t>(S, W, stats, dY, dR, dX, dW, dB, rows, hidden, kind, partial, st);
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+}  // extern "C"

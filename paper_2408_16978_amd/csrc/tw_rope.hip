@@ -1,0 +1,258 @@
+// Rotary positions and the split of the QKV product (include/fpdt_tokenwise.h: fpdt_tw_rope_*).
+//
+// Channels (a, b) of a pair i at position p become A (a cos t - b sin t, b cos t + a sin t), t = p f_i; the gradient is
+// the same with -t.  Every element is read once and written once: bound by the memory.
+//
+// The angle is formed in 64 bits (at 2M tokens a 32-bit product is off by 0.1 rad), turned into turns and reduced to an
+// eighth of a turn there; sine and cosine of what is left are polynomials in 32 bits.  That is about 30 instructions a
+// pair, so a thread keeps its pairs' sines and cosines for all heads of its token: no table is read.
+#include <cmath>
+
+#include "../../include/fpdt_tokenwise.h"
+#include "tw_common.h"
+
+namespace {
+
+using namespace fpdt_tw;
+
+struct RopeArgs {
+    const void* in[3];   // Q, K, V
+    void* out[3];
+    int64_t in_row[3], out_row[3];  // elements from a token to the next
+    int heads[3];
+    const int64_t* positions;
+    int64_t position0, rows;
+    const double* freqs;
+    float amplitude, sign;  // sign: -1 in the backward
+    int D, rot;
+    int slots, tokens;  // slots of a head, tokens of a workgroup
+    int split;          // heads of a workgroup (of all three tensors together)
+};
+
+// sin and cos of 2 pi x, times `amplitude`.  x is reduced to within 1/8 of a multiple of 1/4 in 64 bits; the remainders of
+// the Taylor series up to z^9 and z^10 at z = pi / 4 are below 2e-9 and 2e-10.
+__device__ __forceinline__ void sincos_turns(double x, float amplitude, float& s, float& c)
+{
+    x -= rint(x);
+    const double k = rint(4. * x);
+    const float z = 6.2831853071795864769f * (float)fma(-0.25, k, x), z2 = z * z;
+    const float ps = fmaf(z * z2, fmaf(z2, fmaf(z2, fmaf(z2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), z);
+    const float pc = fmaf(z2, fmaf(z2, fmaf(z2, fmaf(z2, fmaf(z2, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
+    const int q = (int)k & 3;  // quarter turns
+    const float ss = q & 1 ? pc : ps, cc = q & 1 ? ps : pc;
+    s = amplitude * (q & 2 ? -ss : ss);
+    c = amplitude * ((q + 1) & 2 ? -cc : cc);
+}
+
+// A slot of a head: V pairs in two accesses of V elements (halves; both layouts at V = 1), V / 2 pairs in one access
+// (interleaved, V > 1), and behind the rotated channels V elements that are copied.
+template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
+{
+    constexpr bool ONE = INTERLEAVED && V > 1;
+    constexpr int PAIRS = ONE ? V / 2 : V, ACC = ONE ? 1 : 2, U = 4;
+    const int turning = ONE ? a.rot / V : a.rot / 2 / V;
+    const int lane = threadIdx.x / a.slots;  // token of the workgroup
+    const int h0 = blockIdx.y * a.split;
+    for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.rows; t0 += (int64_t)gridDim.x * a.tokens) {
+        const int64_t row = t0 + lane;
+        if (lane >= a.tokens || row >= a.rows) continue;
+        const int64_t pos = a.positions ? a.positions[row] : a.position0 + row;
+        for (int j = threadIdx.x - lane * a.slots; j < a.slots; j += 256) {
+            const bool turns = j < turning;
+            float sn[PAIRS], cs[PAIRS];
+            int at[2];
+            if (turns) {
+                at[0] = (INTERLEAVED && V == 1 ? 2 : 1) * j * V;
+                at[1] = INTERLEAVED ? at[0] + 1 : at[0] + a.rot / 2;
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    const double angle = (double)pos * a.freqs[j * PAIRS + i];
+                    sincos_turns(angle * 0.15915494309189533577, a.amplitude, sn[i], cs[i]);
+                    sn[i] *= a.sign;
+                }
+            } else {
+                at[0] = at[1] = a.rot + (j - turning) * V;
+            }
+            int before = 0;
+#pragma unroll
+            for (int t = 0; t < 3; ++t) {
+                // heads [from, to) of this tensor belong to the workgroup
+                const int from = max(h0 - before, 0), to = min(h0 + a.split - before, a.heads[t]);
+                before += a.heads[t];
+                const bool turn = turns && t < 2;
+                const T* in = static_cast<const T*>(a.in[t]) + row * a.in_row[t];
+                T* out = static_cast<T*>(a.out[t]) + row * a.out_row[t];
+                for (int h = from; h < to; h += U) {
+                    Vec<T, V> x[U][ACC];
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int c = 0; c < ACC; ++c)
+                            if (h + u < to && (c == 0 || turns)) x[u][c] = load<V>(in + (int64_t)(h + u) * a.D + at[c]);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (h + u >= to) break;
+                        if (turn) {
+                            float y[ACC * V];
+#pragma unroll
+                            for (int i = 0; i < PAIRS; ++i) {
+                                const int ia = ONE ? 2 * i : i, ib = ONE ? 2 * i + 1 : V + i;
+                                const float p = to_float(x[u][0].e[ia]), q = to_float(x[u][ib / V].e[ib % V]);
+                                y[ia] = fmaf(p, cs[i], -q * sn[i]);
+                                y[ib] = fmaf(q, cs[i], p * sn[i]);
+                            }
+#pragma unroll
+                            for (int c = 0; c < ACC; ++c) x[u][c] = rounded<V>(y + c * V, T());
+                        }
+#pragma unroll
+                        for (int c = 0; c < ACC; ++c)
+                            if (c == 0 || turns) store(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
+                    }
+                }
+            }
+        }
+    }
+}
+
+constexpr int MOST_D = 8192, MOST_HEADS = 4096;
+
+template <class T, int V> void launch_v(const RopeArgs& a, bool interleaved, dim3 grid, hipStream_t st)
+{
+    if (interleaved) rope_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
+    else rope_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+}
+
+// The widest access whose elements are all turned or all copied, in either half.
+int access(int D, int rot, bool interleaved, int most)
+{
+    int v = most;
+    while (v > 1 && ((interleaved ? rot : rot / 2) % v || (D - rot) % v)) v /= 2;
+    return v;
+}
+
+// Do two tensors of rows of `wa` and `wb` bytes, `ra` and `rb` bytes apart, share a byte?  Rows of one distance may lie
+// between each other; with two distances, ranges that meet count as shared.
+bool rows_meet(const void* a, int64_t ra, int64_t wa, const void* b, int64_t rb, int64_t wb, int64_t rows)
+{
+    if (!ranges_meet(a, (size_t)((rows - 1) * ra + wa), b, (size_t)((rows - 1) * rb + wb))) return false;
+    if (ra != rb) return rows > 1 || ranges_meet(a, (size_t)wa, b, (size_t)wb);
+    if (rows == 1) return true;
+    const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+    const int64_t m = ((d % ra) + ra) % ra;  // columns from a row of a to the next row of b
+    return m < wa || ra - m < wb;
+}
+
+int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], const int64_t out_row[3], const int64_t* positions, int64_t position0,
+         const double* freqs, float amplitude, int64_t rows, int Hq, int Hkv, int D, int rot, int layout, int dtype, bool back, void* stream)
+{
+    clear_error();
+    static const char* const names = "QKV";
+    if (rows <= 0 || Hq <= 0 || Hkv < 0 || D <= 0) return fail(TW_INVALID, "rows, Hq and D must be positive, Hkv not negative");
+    if (rot <= 0 || rot % 2 || rot > D) return fail(TW_INVALID, "rot=%d must be even and in [2, D]", rot);
+    if (layout != FPDT_TW_ROPE_HALF && layout != FPDT_TW_ROPE_INTERLEAVED) return fail(TW_INVALID, "unknown layout %d", layout);
+    if (dtype != FPDT_TW_F32 && dtype != FPDT_TW_BF16) return fail(TW_INVALID, "unknown dtype %d", dtype);
+    if (!std::isfinite(amplitude)) return fail(TW_INVALID, "amplitude must be finite");
+    if (!freqs || misaligned(freqs, 8) || misaligned(positions, 8)) return fail(TW_INVALID, "freqs NULL, or freqs or positions misaligned");
+    if (D > MOST_D || Hq > MOST_HEADS || Hkv > MOST_HEADS || rows > INT32_MAX) return fail(TW_UNSUPPORTED, "sizes beyond the launch limits");
+    const int size = dtype == FPDT_TW_F32 ? 4 : 2;
+    RopeArgs a = {};
+    for (int t = 0; t < 3; ++t) {
+        const int heads = t == 0 ? Hq : Hkv;
+        if ((in[t] == nullptr) != (out[t] == nullptr)) return fail(TW_INVALID, "%c is given on one side only", names[t]);
+        if (!in[t]) {
+            if (t == 0) return fail(TW_INVALID, "NULL tensor pointer");
+            continue;
+        }
+        if (heads == 0) return fail(TW_INVALID, "%c is given, but Hkv is 0", names[t]);
+        if (in_row[t] < (int64_t)heads * D || out_row[t] < (int64_t)heads * D) return fail(TW_INVALID, "rows of %c are closer than its heads are long", names[t]);
+        if (in_row[t] > (1 << 28) || out_row[t] > (1 << 28)) return fail(TW_UNSUPPORTED, "rows of %c beyond the launch limits", names[t]);
+        if (misaligned(in[t], size) || misaligned(out[t], size)) return fail(TW_INVALID, "%c is not aligned to its elements", names[t]);
+        a.in[t] = in[t], a.out[t] = out[t], a.in_row[t] = in_row[t], a.out_row[t] = out_row[t], a.heads[t] = heads;
+    }
+    // what is written may be what is read at the same place, and nothing else
+    for (int t = 0; t < 3; ++t)
+        for (int u = 0; u < 3; ++u) {
+            const int64_t wt = (int64_t)a.heads[t] * D * size, wu = (int64_t)a.heads[u] * D * size;
+            if (!wt || !wu) continue;
+            const bool same = t == u && a.out[t] == a.in[u] && a.out_row[t] == a.in_row[u];
+            if (!same && rows_meet(a.out[t], a.out_row[t] * size, wt, a.in[u], a.in_row[u] * size, wu, rows))
+                return fail(TW_INVALID, "%c's output overlaps %c's input", names[t], names[u]);
+            if (t < u && rows_meet(a.out[t], a.out_row[t] * size, wt, a.out[u], a.out_row[u] * size, wu, rows))
+                return fail(TW_INVALID, "the outputs of %c and %c overlap", names[t], names[u]);
+        }
+    a.positions = positions, a.position0 = position0, a.rows = rows, a.freqs = freqs, a.amplitude = amplitude, a.sign = back ? -1.f : 1.f;
+    a.D = D, a.rot = rot;
+    const bool inter = layout == FPDT_TW_ROPE_INTERLEAVED;
+    const int v = access(D, rot, inter, 16 / size), heads = a.heads[0] + a.heads[1] + a.heads[2];
+    a.slots = (inter && v > 1 ? rot / v : rot / 2 / v) + (D - rot) / v;
+    a.tokens = a.slots >= 256 ? 1 : 256 / a.slots;
+    const int64_t tiles = (rows + a.tokens - 1) / a.tokens;
+    // All heads of a token in one thread, as long as that leaves every compute unit some workgroups.
+    int parts = tiles >= 1024 ? 1 : (int)((1024 + tiles - 1) / tiles);
+    if (parts > heads) parts = heads;
+    a.split = (heads + parts - 1) / parts;
+    const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((heads + a.split - 1) / a.split));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (size == 4) {
+        if (v == 4) launch_v<float, 4>(a, inter, grid, st);
+        else if (v == 2) launch_v<float, 2>(a, inter, grid, st);
+        else launch_v<float, 1>(a, inter, grid, st);
+    } else {
+        if (v == 8) launch_v<uint16_t, 8>(a, inter, grid, st);
+        else if (v == 4) launch_v<uint16_t, 4>(a, inter, grid, st);
+        else if (v == 2) launch_v<uint16_t, 2>(a, inter, grid, st);
+        else launch_v<uint16_t, 1>(a, inter, grid, st);
+    }
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fpdt_tw_rope_freqs(int rot, double base, int scaling, double factor, double context, double low, double high, double* freqs)
+{
+    clear_error();
+    if (!freqs) return fail(TW_INVALID, "NULL pointer");
+    if (rot <= 0 || rot % 2 || rot > MOST_D) return fail(TW_INVALID, "rot=%d must be even and in [2, %d]", rot, MOST_D);
+    if (!std::isfinite(base) || base <= 0) return fail(TW_INVALID, "base must be finite and positive");
+    if (scaling < FPDT_TW_ROPE_PLAIN || scaling > FPDT_TW_ROPE_PARTS) return fail(TW_INVALID, "unknown scaling %d", scaling);
+    if (scaling != FPDT_TW_ROPE_PLAIN && (!std::isfinite(factor) || factor <= 0)) return fail(TW_INVALID, "factor must be finite and positive");
+    if (scaling == FPDT_TW_ROPE_PARTS && !(std::isfinite(context) && context > 0 && std::isfinite(low) && std::isfinite(high) && low < high))
+        return fail(TW_INVALID, "by parts: context must be positive, and low < high");
+    if (scaling == FPDT_TW_ROPE_RAISED && rot > 2) base *= std::pow(factor, rot / (rot - 2.));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2. * i / rot);
+        if (scaling == FPDT_TW_ROPE_LINEAR) f /= factor;
+        if (scaling == FPDT_TW_ROPE_PARTS) {
+            const double turns = context * f / 6.2831853071795864769;
+            const double keep = std::fmin(1., std::fmax(0., (turns - low) / (high - low)));
+            f = keep * f + (1 - keep) * f / factor;
+        }
+        freqs[i] = f;
+    }
+    return TW_OK;
+}
+
+int fpdt_tw_rope_fwd(const void* Q, int64_t q_row, const void* K, int64_t k_row, const void* V, int64_t v_row, void* Qo, int64_t qo_row, void* Ko,
+                     int64_t ko_row, void* Vo, int64_t vo_row, const int64_t* positions, int64_t position0, const double* freqs, float amplitude,
+                     int64_t rows, int Hq, int Hkv, int D, int rot, int layout, int dtype, void* stream)
+{
+    const void* const in[3] = {Q, K, V};
+    void* const out[3] = {Qo, Ko, Vo};
+    const int64_t in_row[3] = {q_row, k_row, v_row}, out_row[3] = {qo_row, ko_row, vo_row};
+    return rope(in, in_row, out, out_row, positions, position0, freqs, amplitude, rows, Hq, Hkv, D, rot, layout, dtype, false, stream);
+}
+
+int fpdt_tw_rope_bwd(const void* dQo, int64_t qo_row, const void* dKo, int64_t ko_row, const void* dVo, int64_t vo_row, void* dQ, int64_t q_row,
+                     void* dK, int64_t k_row, void* dV, int64_t v_row, const int64_t* positions, int64_t position0, const double* freqs,
+                     float amplitude, int64_t rows, int Hq, int Hkv, int D, int rot, int layout, int dtype, void* stream)
+{
+    const void* const in[3] = {dQo, dKo, dVo};
+    void* const out[3] = {dQ, dK, dV};
+    const int64_t in_row[3] = {qo_row, ko_row, vo_row}, out_row[3] = {q_row, k_row, v_row};
+    return rope(in, in_row, out, out_row, positions, position0, freqs, amplitude, rows, Hq, Hkv, D, rot, layout, dtype, true, stream);
+}
+
+}  // extern "C"
