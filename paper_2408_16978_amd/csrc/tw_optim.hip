@@ -27,7 +27,6 @@ template <class Tensor, int N> struct List {
 // The tensor of a unit: how many tensors begin at it or before.
 template <int N> __device__ __forceinline__ int find(const unsigned (&first)[N], unsigned unit)
 {
-    static_assert(N % 16 == 0, "");
     int n = 0;
 #pragma unroll
     for (int i = 0; i < N; i += 64) {
@@ -37,18 +36,19 @@ template <int N> __device__ __forceinline__ int find(const unsigned (&first)[N],
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
-template <class T, int V> __device__ __forceinline__ Vec<T, V> load_to(const T* p, int64_t left)
+// `left` elements are left at p; WHOLE: at least V.
+template <class T, int V, bool WHOLE> __device__ __forceinline__ Vec<T, V> load_to(const T* p, int64_t left)
 {
-    if (left >= V) return load<V>(p);
+    if (WHOLE || left >= V) return load_once<V>(p);
     Vec<T, V> v;
 #pragma unroll
     for (int e = 0; e < V; ++e) v.e[e] = e < left ? p[e] : T(0);
     return v;
 }
-template <class T, int V> __device__ __forceinline__ void store_to(T* p, int64_t left, const Vec<T, V>& v)
+template <bool WHOLE, class T, int V> __device__ __forceinline__ void store_to(T* p, int64_t left, const Vec<T, V>& v)
 {
-    if (left >= V) {
-        store(p, v);
+    if (WHOLE || left >= V) {
+        store_once(p, v);
         return;
     }
 #pragma unroll
@@ -90,14 +90,16 @@ template <class T> __global__ __launch_bounds__(256) void grad_norm_kernel(NormA
         const int64_t at = (int64_t)(u - a.list.first[k]) * NORM_UNIT, left = a.list.t[k].n - at;
         const T* g = static_cast<const T*>(a.list.t[k].g) + at;
         Vec<T, V> x[N];
+        if (left >= NORM_UNIT) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (i * 256 + threadIdx.x) * V;
-            if (left >= NORM_UNIT) x[i] = load<V>(g + c);
-            else if (c < left) x[i] = load_to<T, V>(g + c, left - c);
-            else
+            for (int i = 0; i < N; ++i) x[i] = load_once<V>(g + (i * 256 + threadIdx.x) * V);
+        } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[i].e[e] = T(0);
+            for (int i = 0; i < N; ++i) {
+                const int c = (i * 256 + threadIdx.x) * V;
+                x[i] = {};
+                if (c < left) x[i] = load_to<T, V, false>(g + c, left - c);
+            }
         }
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -139,7 +141,7 @@ struct Tensor8 : Tensor32 {
     uint8_t *m_exp, *v_exp;
     unsigned ordinal, pad;
 };
-constexpr int TENSORS32 = 48, TENSORS8 = 32;
+constexpr int TENSORS32 = 64, TENSORS8 = 47;  // what 4 KB hold
 
 struct AdamwHyper {
     double lr, bc1, bc2, log1, log2;  // bc = 1 - beta^step; logarithms of the betas
@@ -198,13 +200,41 @@ template <class G> __device__ __forceinline__ void zero_grads(G* g, int64_t left
 #pragma unroll
     for (int i = 0; i < UNIT / 256 / 4; ++i) {
         const int c = (i * 256 + threadIdx.x) * 4;
-        if (c < left) store_to<G, 4>(g + c, left - c, Vec<G, 4>{});
+        if (c < left) store_to<false>(g + c, left - c, Vec<G, 4>{});
+    }
+}
+
+template <class G, bool WHOLE>
+__device__ __forceinline__ void adamw_unit(const Step& s, G* g, float* p, float* m, float* v, uint16_t* w, int64_t left, bool zero)
+{
+    constexpr int V = 4, N = UNIT / 256 / V;
+    Vec<G, V> xg[N];
+    Vec<float, V> xp[N], xm[N], xv[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 256 + threadIdx.x) * V;
+        if (!WHOLE && c >= left) break;
+        xg[i] = load_to<G, V, WHOLE>(g + c, left - c);
+        xp[i] = load_to<float, V, WHOLE>(p + c, left - c);
+        xm[i] = load_to<float, V, WHOLE>(m + c, left - c);
+        xv[i] = load_to<float, V, WHOLE>(v + c, left - c);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 256 + threadIdx.x) * V;
+        if (!WHOLE && c >= left) break;
+#pragma unroll
+        for (int e = 0; e < V; ++e) update(s, to_float(xg[i].e[e]), xp[i].e[e], xm[i].e[e], xv[i].e[e]);
+        store_to<WHOLE>(p + c, left - c, xp[i]);
+        store_to<WHOLE>(m + c, left - c, xm[i]);
+        store_to<WHOLE>(v + c, left - c, xv[i]);
+        if (w) store_to<WHOLE>(w + c, left - c, rounded<V>(xp[i].e, uint16_t()));
+        if (zero) store_to<WHOLE>(g + c, left - c, Vec<G, V>{});
     }
 }
 
 template <class G> __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<Tensor32, TENSORS32> a)
 {
-    constexpr int V = 4, N = UNIT / 256 / V;
     const int k = find(a.list.first, blockIdx.x);
     const Tensor32& t = a.list.t[k];
     const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
@@ -214,31 +244,10 @@ template <class G> __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs
         if (a.h.zero) zero_grads(g, left);
         return;
     }
-    float *p = t.p + at, *m = static_cast<float*>(t.m) + at, *v = static_cast<float*>(t.v) + at;
+    float *m = static_cast<float*>(t.m) + at, *v = static_cast<float*>(t.v) + at;
     uint16_t* w = t.w ? t.w + at : nullptr;
-    Vec<G, V> xg[N];
-    Vec<float, V> xp[N], xm[N], xv[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = (i * 256 + threadIdx.x) * V;
-        if (c >= left) break;
-        xg[i] = load_to<G, V>(g + c, left - c);
-        xp[i] = load_to<float, V>(p + c, left - c);
-        xm[i] = load_to<float, V>(m + c, left - c);
-        xv[i] = load_to<float, V>(v + c, left - c);
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = (i * 256 + threadIdx.x) * V;
-        if (c >= left) break;
-#pragma unroll
-        for (int e = 0; e < V; ++e) update(s, to_float(xg[i].e[e]), xp[i].e[e], xm[i].e[e], xv[i].e[e]);
-        store_to(p + c, left - c, xp[i]);
-        store_to(m + c, left - c, xm[i]);
-        store_to(v + c, left - c, xv[i]);
-        if (w) store_to(w + c, left - c, rounded<V>(xp[i].e, uint16_t()));
-        if (a.h.zero) store_to(g + c, left - c, Vec<G, V>{});
-    }
+    if (left >= UNIT) adamw_unit<G, true>(s, g, t.p + at, m, v, w, left, a.h.zero);
+    else adamw_unit<G, false>(s, g, t.p + at, m, v, w, left, a.h.zero);
 }
 
 // ---- 8-bit states.  A block of 128 has an exponent byte E, that of its largest value rounded up to three fraction bits (at
@@ -290,9 +299,78 @@ template <int D> __device__ __forceinline__ unsigned encode(float x, unsigned ex
     return exp == 255 ? 0 : code;
 }
 
-template <class G> __global__ __launch_bounds__(256) void adamw8_kernel(AdamwArgs<Tensor8, TENSORS8> a)
+template <class G, bool WHOLE>
+__device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8_t* m, uint8_t* v, uint8_t* me, uint8_t* ve, uint16_t* w, unsigned at,
+                                            unsigned key, int64_t left, bool zero)
 {
     constexpr int V = 8, N = UNIT / 256 / V;
+    Vec<G, V> xg[N];
+    Vec<float, V / 2> xp[N][2];
+    Vec<uint8_t, V> xm[N], xv[N];
+    unsigned em[N], ev[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 256 + threadIdx.x) * V;
+        if (WHOLE || c < left) {
+            if constexpr (sizeof(G) == 4) {
+                const Vec<G, V / 2> a = load_to<G, V / 2, WHOLE>(g + c, left - c), b = load_to<G, V / 2, WHOLE>(g + c + V / 2, left - c - V / 2);
+#pragma unroll
+                for (int e = 0; e < V; ++e) xg[i].e[e] = e < V / 2 ? a.e[e % (V / 2)] : b.e[e % (V / 2)];
+            } else {
+                xg[i] = load_to<G, V, WHOLE>(g + c, left - c);
+            }
+            xp[i][0] = load_to<float, V / 2, WHOLE>(p + c, left - c);
+            xp[i][1] = load_to<float, V / 2, WHOLE>(p + c + V / 2, left - c - V / 2);
+            xm[i] = load_to<uint8_t, V, WHOLE>(m + c, left - c);
+            xv[i] = load_to<uint8_t, V, WHOLE>(v + c, left - c);
+            em[i] = me[c / BLOCK], ev[i] = ve[c / BLOCK];
+        } else {  // no element: zeros, which do not count in the block's largest
+            xg[i] = {}, xp[i][0] = xp[i][1] = {}, xm[i] = {}, xv[i] = {}, em[i] = ev[i] = 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 256 + threadIdx.x) * V;
+        float fm[V], fv[V];
+        unsigned most_m = 0, most_v = 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            fm[e] = decode<15>(xm[i].e[e], em[i]), fv[e] = decode<31>(xv[i].e[e], ev[i]);
+            update(s, to_float(xg[i].e[e]), xp[i][e / (V / 2)].e[e % (V / 2)], fm[e], fv[e]);
+            if (WHOLE || c + e < left) {  // (a NaN of the block's exponent must not come from behind the end)
+                most_m = max(most_m, __float_as_uint(fm[e]) & 0x7fffffffu);
+                most_v = max(most_v, __float_as_uint(fv[e]) & 0x7fffffffu);
+            }
+        }
+        const unsigned nm = exponent(block_max(most_m)), nv = exponent(block_max(most_v));
+        if (!WHOLE && c >= left) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const unsigned random = mix((at + c + e) * 0x9E3779B1u ^ key);
+            xm[i].e[e] = (uint8_t)encode<15>(fm[e], nm, random & 0xffff);
+            xv[i].e[e] = (uint8_t)encode<31>(fv[e], nv, random >> 16);
+        }
+        store_to<WHOLE>(m + c, left - c, xm[i]);
+        store_to<WHOLE>(v + c, left - c, xv[i]);
+        if (c % BLOCK == 0) me[c / BLOCK] = (uint8_t)nm, ve[c / BLOCK] = (uint8_t)nv;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int d = c + h * (V / 2);
+            if (!WHOLE && d >= left) break;
+            store_to<WHOLE>(p + d, left - d, xp[i][h]);
+            if (zero) store_to<WHOLE>(g + d, left - d, Vec<G, V / 2>{});
+        }
+        if (w) {
+            float all[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) all[e] = xp[i][e / (V / 2)].e[e % (V / 2)];
+            store_to<WHOLE>(w + c, left - c, rounded<V>(all, uint16_t()));
+        }
+    }
+}
+
+template <class G> __global__ __launch_bounds__(256) void adamw8_kernel(AdamwArgs<Tensor8, TENSORS8> a)
+{
     const int k = find(a.list.first, blockIdx.x);
     const Tensor8& t = a.list.t[k];
     const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
@@ -304,56 +382,10 @@ template <class G> __global__ __launch_bounds__(256) void adamw8_kernel(AdamwArg
     }
     unsigned key = mix(mix(mix(a.h.seed ^ 0x243F6A88u) ^ (unsigned)s.step * 0x9E3779B1u) ^ t.ordinal * 0x85A308D3u);
     if (at >> 32) key = mix(key + (unsigned)(at >> 32));
-    float* p = t.p + at;
-    uint8_t *m = static_cast<uint8_t*>(t.m) + at, *v = static_cast<uint8_t*>(t.v) + at;
-    uint8_t *me = t.m_exp + at / BLOCK, *ve = t.v_exp + at / BLOCK;
+    uint8_t *m = static_cast<uint8_t*>(t.m) + at, *v = static_cast<uint8_t*>(t.v) + at, *me = t.m_exp + at / BLOCK, *ve = t.v_exp + at / BLOCK;
     uint16_t* w = t.w ? t.w + at : nullptr;
-    Vec<G, V> xg[N];
-    Vec<float, V> xp[N];
-    Vec<uint8_t, V> xm[N], xv[N];
-    unsigned em[N], ev[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = (i * 256 + threadIdx.x) * V;
-        if (c < left) {
-            xg[i] = load_to<G, V>(g + c, left - c);
-            xp[i] = load_to<float, V>(p + c, left - c);
-            xm[i] = load_to<uint8_t, V>(m + c, left - c);
-            xv[i] = load_to<uint8_t, V>(v + c, left - c);
-            em[i] = me[c / BLOCK], ev[i] = ve[c / BLOCK];
-        } else {  // no element: zeros, which do not count in the block's largest
-            xg[i] = {}, xp[i] = {}, xm[i] = {}, xv[i] = {}, em[i] = ev[i] = 0;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = (i * 256 + threadIdx.x) * V;
-        float fm[V], fv[V];
-        unsigned most_m = 0, most_v = 0;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            fm[e] = decode<15>(xm[i].e[e], em[i]), fv[e] = decode<31>(xv[i].e[e], ev[i]);
-            update(s, to_float(xg[i].e[e]), xp[i].e[e], fm[e], fv[e]);
-            if (c + e < left) {  // (a NaN of the block's exponent must not come from behind the end)
-                most_m = max(most_m, __float_as_uint(fm[e]) & 0x7fffffffu);
-                most_v = max(most_v, __float_as_uint(fv[e]) & 0x7fffffffu);
-            }
-        }
-        const unsigned nm = exponent(block_max(most_m)), nv = exponent(block_max(most_v));
-        if (c >= left) continue;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const unsigned random = mix((unsigned)(at + c + e) * 0x9E3779B1u ^ key);
-            xm[i].e[e] = (uint8_t)encode<15>(fm[e], nm, random & 0xffff);
-            xv[i].e[e] = (uint8_t)encode<31>(fv[e], nv, random >> 16);
-        }
-        store_to(p + c, left - c, xp[i]);
-        store_to(m + c, left - c, xm[i]);
-        store_to(v + c, left - c, xv[i]);
-        if (c % BLOCK == 0) me[c / BLOCK] = (uint8_t)nm, ve[c / BLOCK] = (uint8_t)nv;
-        if (w) store_to(w + c, left - c, rounded<V>(xp[i].e, uint16_t()));
-        if (a.h.zero) store_to(g + c, left - c, Vec<G, V>{});
-    }
+    if (left >= UNIT) adamw8_unit<G, true>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
+    else adamw8_unit<G, false>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
 }
 
 struct Unpacked {
@@ -367,25 +399,38 @@ struct UnpackArgs {
 };
 
 // Four significant bits: bfloat16 holds them, in the upper half of the float's bits.
-__global__ __launch_bounds__(256) void adamw_unpack_kernel(UnpackArgs a)
+template <bool WHOLE> __device__ __forceinline__ void unpack_unit(const Unpacked& t, int64_t at, int64_t left)
 {
     constexpr int V = 8, N = UNIT / 256 / V;
-    const int k = find(a.list.first, blockIdx.x);
-    const Unpacked& t = a.list.t[k];
-    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
+    Vec<uint8_t, V> m[N], v[N];
+    unsigned em[N], ev[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int c = (i * 256 + threadIdx.x) * V;
-        if (c >= left) break;
-        const unsigned em = t.m_exp[(at + c) / BLOCK], ev = t.v_exp[(at + c) / BLOCK];
-        const Vec<uint8_t, V> m = load_to<uint8_t, V>(t.m + at + c, left - c), v = load_to<uint8_t, V>(t.v + at + c, left - c);
+        if (!WHOLE && c >= left) break;
+        m[i] = load_to<uint8_t, V, WHOLE>(t.m + at + c, left - c), v[i] = load_to<uint8_t, V, WHOLE>(t.v + at + c, left - c);
+        em[i] = t.m_exp[(at + c) / BLOCK], ev[i] = t.v_exp[(at + c) / BLOCK];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 256 + threadIdx.x) * V;
+        if (!WHOLE && c >= left) break;
         Vec<uint16_t, V> ym, yv;
 #pragma unroll
         for (int e = 0; e < V; ++e)
-            ym.e[e] = (uint16_t)(__float_as_uint(decode<15>(m.e[e], em)) >> 16), yv.e[e] = (uint16_t)(__float_as_uint(decode<31>(v.e[e], ev)) >> 16);
-        store_to(t.m_value + at + c, left - c, ym);
-        store_to(t.v_value + at + c, left - c, yv);
+            ym.e[e] = (uint16_t)(__float_as_uint(decode<15>(m[i].e[e], em[i])) >> 16), yv.e[e] = (uint16_t)(__float_as_uint(decode<31>(v[i].e[e], ev[i])) >> 16);
+        store_to<WHOLE>(t.m_value + at + c, left - c, ym);
+        store_to<WHOLE>(t.v_value + at + c, left - c, yv);
     }
+}
+
+__global__ __launch_bounds__(256) void adamw_unpack_kernel(UnpackArgs a)
+{
+    const int k = find(a.list.first, blockIdx.x);
+    const Unpacked& t = a.list.t[k];
+    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
+    if (left >= UNIT) unpack_unit<true>(t, at, left);
+    else unpack_unit<false>(t, at, left);
 }
 
 // ---- host
