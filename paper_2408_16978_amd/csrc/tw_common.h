@@ -39,6 +39,7 @@ typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
     template <> struct Raw<BYTES, ALIGN> {                             \
         typedef TYPE type __attribute__((aligned(ALIGN), may_alias));  \
     };
+FPDT_TW_RAW(4, 1, unsigned)
 FPDT_TW_RAW(8, 1, uintx2)
 FPDT_TW_RAW(2, 2, uint16_t)
 FPDT_TW_RAW(4, 2, unsigned)

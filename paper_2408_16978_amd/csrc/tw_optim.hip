@@ -185,14 +185,18 @@ __device__ __forceinline__ Step make_step(const AdamwHyper& h, double decay)
 }
 
 // One element.  No product is contracted with a sum: the new states are then the same bits as those of separate
-// operations in 32 bits, and so are the codes that they are rounded to.
+// operations in 32 bits, and so are the codes that they are rounded to.  Root and quotient are the hardware's, each right
+// to a step of 2^-23 (a move of p by 3 of them, at most, of itself): with 8-bit states their correctly rounded
+// forms made a third of all instructions, and these bound the step.  A v that is no normal number counts as the smallest, which
+// the hardware's root would take for zero.
 __device__ __forceinline__ void update(const Step& s, float g, float& p, float& m, float& v)
 {
 #pragma clang fp contract(off)
     g = g * s.scale;
     m = m * s.b1 + g * s.c1;
     v = v * s.b2 + g * g * s.c2;
-    p = p * s.keep - m * s.rate / (sqrtf(v) * s.root + s.eps);
+    const float root = __builtin_amdgcn_sqrtf(v < 0x1p-126f ? 0x1p-126f : v) * s.root + s.eps;
+    p = p * s.keep - m * s.rate * __builtin_amdgcn_rcpf(root);
 }
 
 template <class G> __device__ __forceinline__ void zero_grads(G* g, int64_t left)
@@ -263,21 +267,25 @@ __device__ __forceinline__ unsigned mix(unsigned x)
     return x ^ (x >> 16);
 }
 
-template <int D> __device__ __forceinline__ float decode(unsigned code, unsigned exp)
+// `nan`: 0x7fc00000 where the block's byte is 255, else 0
+template <int D> __device__ __forceinline__ float decode(unsigned code, unsigned base, unsigned nan)
 {
     const unsigned mag = D == 15 ? code & 127 : code;
-    unsigned bits = mag ? ((exp - D) << 23) + (mag << 20) : 0;
-    if (exp == 255) bits = 0x7fc00000u;
-    return __uint_as_float(D == 15 ? bits | (code & 128) << 24 : bits);
+    const unsigned bits = mag ? base + (mag << 20) : 0;
+    return __uint_as_float(bits | nan | (D == 15 ? (code & 128) << 24 : 0));
 }
+template <int D> __device__ __forceinline__ unsigned decode_base(unsigned exp) { return (exp - D) << 23; }
+__device__ __forceinline__ unsigned decode_nan(unsigned exp) { return exp == 255 ? 0x7fc00000u : 0; }
 
-// The largest over the 16 lanes of a block, in each of them.
+// The largest over the 32 lanes of a block, in each of them: rotated by 8, 4, 2 and 1 of 16 lanes, then with the other 16.
 __device__ __forceinline__ unsigned block_max(unsigned x)
 {
-    x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true));  // rotated by 8 of 16 lanes
+    x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true));
     x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, true));
     x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
-    return max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
+    x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
+    const auto both = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return max(both[0], both[1]);
 }
 __device__ __forceinline__ unsigned exponent(unsigned most)
 {
@@ -288,44 +296,43 @@ __device__ __forceinline__ unsigned exponent(unsigned most)
 // |x| rounded to a code, up with the probability of what is cut off (16 random bits): a step changes v by 1 - beta2 of
 // itself, far less than half the distance of two codes, and rounded to nearest it would stay where it is.  What is below code
 // 1 becomes 1 or 0 likewise for m, and 1 for v, by which a step divides.
-template <int D> __device__ __forceinline__ unsigned encode(float x, unsigned exp, unsigned random16)
+// (both cases computed, one taken: a branch for each element kept them from overlapping)
+__device__ __forceinline__ unsigned encode_m(float x, unsigned base, float least, unsigned random16)
 {
     const unsigned bits = __float_as_uint(x) & 0x7fffffffu;
-    const unsigned base = (exp - D) << 3;
-    const float least = __uint_as_float((base + 1) << 20), size = __uint_as_float(bits);
-    const unsigned low = D == 15 ? (float)random16 * 0x1p-16f * least < size : size > 0.f;
-    unsigned code = size >= least ? ((bits + (random16 << 4)) >> 20) - base : low;
-    if (D == 15 && x < 0.f) code |= 128;
-    return exp == 255 ? 0 : code;
+    const float size = __uint_as_float(bits);
+    const unsigned low = (float)random16 * (0x1p-16f * least) < size, high = ((bits + (random16 << 4)) >> 20) - base;
+    const unsigned code = __builtin_unpredictable(size >= least) ? high : low;
+    return code | (__float_as_uint(x) >> 24 & 128);
+}
+__device__ __forceinline__ unsigned encode_v(float x, unsigned base, unsigned random16)
+{
+    const unsigned bits = __float_as_uint(x);
+    return (unsigned)max((int)((bits + (random16 << 4)) >> 20) - (int)base, (int)min(bits, 1u));  // (v is not negative)
 }
 
+// Four elements of a lane at a time, so that every access of a wave is contiguous (with eight, the two halves of a lane's p
+// and g are 32 bytes from the next lane's).
 template <class G, bool WHOLE>
 __device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8_t* m, uint8_t* v, uint8_t* me, uint8_t* ve, uint16_t* w, unsigned at,
                                             unsigned key, int64_t left, bool zero)
 {
-    constexpr int V = 8, N = UNIT / 256 / V;
+    constexpr int V = 4, N = UNIT / 256 / V;
     Vec<G, V> xg[N];
-    Vec<float, V / 2> xp[N][2];
+    Vec<float, V> xp[N];
     Vec<uint8_t, V> xm[N], xv[N];
     unsigned em[N], ev[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int c = (i * 256 + threadIdx.x) * V;
         if (WHOLE || c < left) {
-            if constexpr (sizeof(G) == 4) {
-                const Vec<G, V / 2> a = load_to<G, V / 2, WHOLE>(g + c, left - c), b = load_to<G, V / 2, WHOLE>(g + c + V / 2, left - c - V / 2);
-#pragma unroll
-                for (int e = 0; e < V; ++e) xg[i].e[e] = e < V / 2 ? a.e[e % (V / 2)] : b.e[e % (V / 2)];
-            } else {
-                xg[i] = load_to<G, V, WHOLE>(g + c, left - c);
-            }
-            xp[i][0] = load_to<float, V / 2, WHOLE>(p + c, left - c);
-            xp[i][1] = load_to<float, V / 2, WHOLE>(p + c + V / 2, left - c - V / 2);
+            xg[i] = load_to<G, V, WHOLE>(g + c, left - c);
+            xp[i] = load_to<float, V, WHOLE>(p + c, left - c);
             xm[i] = load_to<uint8_t, V, WHOLE>(m + c, left - c);
             xv[i] = load_to<uint8_t, V, WHOLE>(v + c, left - c);
             em[i] = me[c / BLOCK], ev[i] = ve[c / BLOCK];
         } else {  // no element: zeros, which do not count in the block's largest
-            xg[i] = {}, xp[i][0] = xp[i][1] = {}, xm[i] = {}, xv[i] = {}, em[i] = ev[i] = 0;
+            xg[i] = {}, xp[i] = {}, xm[i] = {}, xv[i] = {}, em[i] = ev[i] = 0;
         }
     }
 #pragma unroll
@@ -335,8 +342,9 @@ __device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8
         unsigned most_m = 0, most_v = 0;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            fm[e] = decode<15>(xm[i].e[e], em[i]), fv[e] = decode<31>(xv[i].e[e], ev[i]);
-            update(s, to_float(xg[i].e[e]), xp[i][e / (V / 2)].e[e % (V / 2)], fm[e], fv[e]);
+            fm[e] = decode<15>(xm[i].e[e], decode_base<15>(em[i]), decode_nan(em[i]));
+            fv[e] = decode<31>(xv[i].e[e], decode_base<31>(ev[i]), decode_nan(ev[i]));
+            update(s, to_float(xg[i].e[e]), xp[i].e[e], fm[e], fv[e]);
             if (WHOLE || c + e < left) {  // (a NaN of the block's exponent must not come from behind the end)
                 most_m = max(most_m, __float_as_uint(fm[e]) & 0x7fffffffu);
                 most_v = max(most_v, __float_as_uint(fv[e]) & 0x7fffffffu);
@@ -344,28 +352,22 @@ __device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8
         }
         const unsigned nm = exponent(block_max(most_m)), nv = exponent(block_max(most_v));
         if (!WHOLE && c >= left) continue;
+        const unsigned base_m = (nm - 15) << 3, base_v = (nv - 31) << 3;
+        const float least = __uint_as_float((base_m + 1) << 20);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const unsigned random = mix((at + c + e) * 0x9E3779B1u ^ key);
-            xm[i].e[e] = (uint8_t)encode<15>(fm[e], nm, random & 0xffff);
-            xv[i].e[e] = (uint8_t)encode<31>(fv[e], nv, random >> 16);
+            xm[i].e[e] = (uint8_t)encode_m(fm[e], base_m, least, random & 0xffff);
+            xv[i].e[e] = (uint8_t)encode_v(fv[e], base_v, random >> 16);
         }
+        if (nm == 255) xm[i] = {};
+        if (nv == 255) xv[i] = {};
         store_to<WHOLE>(m + c, left - c, xm[i]);
         store_to<WHOLE>(v + c, left - c, xv[i]);
         if (c % BLOCK == 0) me[c / BLOCK] = (uint8_t)nm, ve[c / BLOCK] = (uint8_t)nv;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int d = c + h * (V / 2);
-            if (!WHOLE && d >= left) break;
-            store_to<WHOLE>(p + d, left - d, xp[i][h]);
-            if (zero) store_to<WHOLE>(g + d, left - d, Vec<G, V / 2>{});
-        }
-        if (w) {
-            float all[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) all[e] = xp[i][e / (V / 2)].e[e % (V / 2)];
-            store_to<WHOLE>(w + c, left - c, rounded<V>(all, uint16_t()));
-        }
+        store_to<WHOLE>(p + c, left - c, xp[i]);
+        if (zero) store_to<WHOLE>(g + c, left - c, Vec<G, V>{});
+        if (w) store_to<WHOLE>(w + c, left - c, rounded<V>(xp[i].e, uint16_t()));
     }
 }
 
@@ -418,7 +420,8 @@ template <bool WHOLE> __device__ __forceinline__ void unpack_unit(const Unpacked
         Vec<uint16_t, V> ym, yv;
 #pragma unroll
         for (int e = 0; e < V; ++e)
-            ym.e[e] = (uint16_t)(__float_as_uint(decode<15>(m[i].e[e], em[i])) >> 16), yv.e[e] = (uint16_t)(__float_as_uint(decode<31>(v[i].e[e], ev[i])) >> 16);
+            ym.e[e] = (uint16_t)(__float_as_uint(decode<15>(m[i].e[e], decode_base<15>(em[i]), decode_nan(em[i]))) >> 16),
+            yv.e[e] = (uint16_t)(__float_as_uint(decode<31>(v[i].e[e], decode_base<31>(ev[i]), decode_nan(ev[i]))) >> 16);
         store_to<WHOLE>(t.m_value + at + c, left - c, ym);
         store_to<WHOLE>(t.v_value + at + c, left - c, yv);
     }
