@@ -6,6 +6,7 @@
 //
 // Bound by the memory: a row stays in the registers of the lanes that read it, so each tensor is read or written once.
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/fpdt_tokenwise.h"
 #include "tw_common.h"
@@ -43,33 +44,51 @@ template <int LANES, int N> struct RowSum {
     }
 };
 
-// Access i of a lane covers columns [c, c + V), c = (i LANES + lane) V; the last one of a row may be cut off.
-template <class T, int V> __device__ __forceinline__ Vec<T, V> load_cut(const T* p, int c, int hidden)
+// Access i of a lane covers columns [c, c + V), c = (i LANES + lane) V.  WHOLE: hidden is a multiple of V; if not, the last
+// access of a row is cut off, and rows begin anywhere in a cache line: what is written then goes through the caches, which put
+// the parts of a line together.
+template <bool WHOLE, int V, class T> __device__ __forceinline__ Vec<T, V> load_cut(const T* p, int c, int hidden)
 {
-    if (c + V <= hidden) return load<V>(p + c);
+    if (WHOLE || c + V <= hidden) return load_once<V>(p + c);
     Vec<T, V> v;
 #pragma unroll
     for (int e = 0; e < V; ++e) v.e[e] = c + e < hidden ? p[c + e] : T(0);
     return v;
 }
-template <class T, int V> __device__ __forceinline__ void store_cut(T* p, int c, int hidden, const Vec<T, V>& v)
+template <bool WHOLE, int V, class T> __device__ __forceinline__ void store_cut(T* p, int c, int hidden, const Vec<T, V>& v)
 {
-    if (c + V <= hidden) {
+    if (WHOLE) {
+        store_once(p + c, v);
+    } else if (c + V <= hidden) {
         store(p + c, v);
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-        if (c + e < hidden) p[c + e] = v.e[e];
+        for (int e = 0; e < V; ++e)
+            if (c + e < hidden) p[c + e] = v.e[e];
+    }
+}
+// What all rows share: kept by the caches.
+template <bool WHOLE, int V, class T> __device__ __forceinline__ Vec<T, V> load_row(const T* p, int c, int hidden)
+{
+    if (WHOLE || c + V <= hidden) return load<V>(p + c);
+    return load_cut<WHOLE, V>(p, c, hidden);
 }
 
-// Rows of LANES threads, NA accesses of V elements each; max(LANES, 256) threads.
-template <class T, int LANES, int NA, bool LAYER>
-__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats,
-                                                                               int64_t rows, int hidden, float eps)
+// What was made of v so far is not kept: it is made again from v, which for bf16 takes half the registers.
+template <class T, int V> __device__ __forceinline__ void forget(Vec<T, V>& v)
+{
+    unsigned x[sizeof v / 4];
+    __builtin_memcpy(x, &v, sizeof v);
+#pragma unroll
+    for (unsigned& word : x) asm volatile("" : "+v"(word));
+    __builtin_memcpy(&v, x, sizeof v);
+}
+
+template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
+__device__ __forceinline__ void norm_fwd(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats, int64_t rows, int hidden, float eps,
+                                         float (*red)[1][16])
 {
     constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES;
-    __shared__ float red[2][1][16];
     RowSum<LANES, 1> sum{red};
     const int lane = threadIdx.x % LANES;
     const float inv = 1.f / hidden;
@@ -77,33 +96,27 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(c
         const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
         if (row >= rows) break;  // (only where rows are lanes of a wave: no barrier is left out)
         Vec<T, V> x[NA], r[NA];
-        float s[NA][V];
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int c = (i * LANES + lane) * V;
-            if (c < hidden) x[i] = load_cut<T, V>(X + at, c, hidden);
+            x[i] = {};
+            if (c < hidden) x[i] = load_cut<WHOLE, V>(X + at, c, hidden);
         }
-        if (R)
+        if (R) {
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
                 const int c = (i * LANES + lane) * V;
-                if (c < hidden) r[i] = load_cut<T, V>(R + at, c, hidden);
+                if (c < hidden) r[i] = load_cut<WHOLE, V>(R + at, c, hidden);
             }
 #pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
-            if (c < hidden) {
-                if (R) {
+            for (int i = 0; i < NA; ++i) {
+                const int c = (i * LANES + lane) * V;
+                if (c >= hidden) continue;
+                float s[V];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) s[i][e] = to_float(x[i].e[e]) + to_float(r[i].e[e]);
-                    x[i] = rounded<V>(s[i], T());  // what the backward reads is what is normalised
-                    if (S) store_cut<T, V>(S + at, c, hidden, x[i]);
-                }
-#pragma unroll
-                for (int e = 0; e < V; ++e) s[i][e] = to_float(x[i].e[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) s[i][e] = 0.f;
+                for (int e = 0; e < V; ++e) s[e] = to_float(x[i].e[e]) + to_float(r[i].e[e]);
+                x[i] = rounded<V>(s, T());  // what the backward reads is what is normalised
+                if (S) store_cut<WHOLE, V>(S + at, c, hidden, x[i]);
             }
         }
         float mean = 0.f;
@@ -112,7 +125,7 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(c
 #pragma unroll
             for (int i = 0; i < NA; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[0] += s[i][e];
+                for (int e = 0; e < V; ++e) v[0] += to_float(x[i].e[e]);
             sum(v);
             mean = v[0] * inv;
         }
@@ -120,10 +133,11 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(c
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int c = (i * LANES + lane) * V;
+            if (LAYER && WHOLE && c >= hidden) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                if (LAYER) s[i][e] = c + e < hidden ? s[i][e] - mean : 0.f;
-                v[0] = fmaf(s[i][e], s[i][e], v[0]);
+                const float d = LAYER && !WHOLE && c + e >= hidden ? 0.f : to_float(x[i].e[e]) - mean;
+                v[0] = fmaf(d, d, v[0]);
             }
         }
         sum(v);
@@ -136,39 +150,50 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(c
         for (int i = 0; i < NA; ++i) {
             const int c = (i * LANES + lane) * V;
             if (c >= hidden) continue;
-            const Vec<T, V> w = load_cut<T, V>(W, c, hidden);
+            forget(x[i]);
+            float y[V];
+            const Vec<T, V> w = load_row<WHOLE, V>(W, c, hidden);
 #pragma unroll
-            for (int e = 0; e < V; ++e) s[i][e] *= rstd * to_float(w.e[e]);
+            for (int e = 0; e < V; ++e) y[e] = (to_float(x[i].e[e]) - mean) * rstd * to_float(w.e[e]);
             if (LAYER && B) {
-                const Vec<T, V> b = load_cut<T, V>(B, c, hidden);
+                const Vec<T, V> b = load_row<WHOLE, V>(B, c, hidden);
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[i][e] += to_float(b.e[e]);
+                for (int e = 0; e < V; ++e) y[e] += to_float(b.e[e]);
             }
-            store_cut<T, V>(Y + at, c, hidden, rounded<V>(s[i], T()));
+            store_cut<WHOLE, V>(Y + at, c, hidden, rounded<V>(y, T()));
         }
     }
+}
+
+// Rows of LANES threads, NA accesses of V elements each; max(LANES, 256) threads.
+template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
+__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats,
+                                                                               int64_t rows, int hidden, float eps)
+{
+    __shared__ float red[2][1][16];
+    norm_fwd<T, LANES, NA, LAYER, WHOLE>(X, R, W, B, S, Y, stats, rows, hidden, eps, red);
 }
 
 // Groups of LANES threads walk the rows; a thread keeps its columns' shares of dw and db in registers, a workgroup's
 // groups add theirs up in LDS and leave one row of partial sums each for norm_sums_kernel: no atomics, the same order
 // of sums in every call.
-template <class T, int LANES, int NA, bool LAYER>
-__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
-                                                                               float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
+template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
+__device__ __forceinline__ void norm_bwd(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX, float* partial, int64_t rows, int hidden,
+                                         bool want_w, bool want_b, float (*red)[LAYER ? 2 : 1][16], float* lds)
 {
     constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES, N = LAYER ? 2 : 1;
-    __shared__ float red[2][N][16];
     RowSum<LANES, N> sum{red};
     const int lane = threadIdx.x % LANES;
     const float inv = 1.f / hidden;
-    float w[NA][V], dw[NA][V], db[NA][V];
+    Vec<T, V> w[NA];
+    float dw[NA][V], db[NA][V];
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
         const int c = (i * LANES + lane) * V;
-        Vec<T, V> x;
-        if (c < hidden) x = load_cut<T, V>(W, c, hidden);
+        w[i] = {};
+        if (c < hidden) w[i] = load_row<WHOLE, V>(W, c, hidden);
 #pragma unroll
-        for (int e = 0; e < V; ++e) w[i][e] = c < hidden ? to_float(x.e[e]) : 0.f, dw[i][e] = db[i][e] = 0.f;
+        for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
     }
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
@@ -177,29 +202,26 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(c
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int c = (i * LANES + lane) * V;
-            if (c < hidden) x[i] = load_cut<T, V>(S + at, c, hidden), y[i] = load_cut<T, V>(dY + at, c, hidden);
+            x[i] = {}, y[i] = {};
+            if (c < hidden) x[i] = load_cut<WHOLE, V>(S + at, c, hidden), y[i] = load_cut<WHOLE, V>(dY + at, c, hidden);
         }
         if (dR)
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
                 const int c = (i * LANES + lane) * V;
-                if (c < hidden) r[i] = load_cut<T, V>(dR + at, c, hidden);
+                if (c < hidden) r[i] = load_cut<WHOLE, V>(dR + at, c, hidden);
             }
         const float mean = LAYER ? stats[row] : 0.f, rstd = stats[(LAYER ? rows : 0) + row];
         float v[N] = {};
-        float u[NA][V], h[NA][V];
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool in = c + e < hidden;
-                const float dy = in ? to_float(y[i].e[e]) : 0.f;
-                u[i][e] = in ? (to_float(x[i].e[e]) - mean) * rstd : 0.f;
-                h[i][e] = dy * w[i][e];
-                v[0] = fmaf(h[i][e], u[i][e], v[0]);
-                if (LAYER) v[N - 1] += h[i][e], db[i][e] += dy;
-                dw[i][e] = fmaf(dy, u[i][e], dw[i][e]);
+                const float dy = to_float(y[i].e[e]);  // (0 behind the row: whatever u is there counts for nothing)
+                const float u = (to_float(x[i].e[e]) - mean) * rstd, h = dy * to_float(w[i].e[e]);
+                v[0] = fmaf(h, u, v[0]);
+                if (LAYER) v[N - 1] += h, db[i][e] += dy;
+                dw[i][e] = fmaf(dy, u, dw[i][e]);
             }
         }
         sum(v);
@@ -208,16 +230,18 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(c
         for (int i = 0; i < NA; ++i) {
             const int c = (i * LANES + lane) * V;
             if (c >= hidden) continue;
+            forget(x[i]), forget(y[i]), forget(w[i]);
+            float d[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                h[i][e] = rstd * (h[i][e] - level - u[i][e] * along);
-                if (dR) h[i][e] += to_float(r[i].e[e]);
+                const float u = (to_float(x[i].e[e]) - mean) * rstd, h = to_float(y[i].e[e]) * to_float(w[i].e[e]);
+                d[e] = rstd * (h - level - u * along);
+                if (dR) d[e] += to_float(r[i].e[e]);
             }
-            store_cut<T, V>(dX + at, c, hidden, rounded<V>(h[i], T()));
+            store_cut<WHOLE, V>(dX + at, c, hidden, rounded<V>(d, T()));
         }
     }
     if (!want_w && !want_b) return;
-    __shared__ float lds[ROWS > 1 ? ROWS : 1][ROWS > 1 ? NA * V * LANES : 1];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         if (k == 0 ? !want_w : !want_b) continue;
@@ -228,12 +252,12 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(c
 #pragma unroll
             for (int i = 0; i < NA; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) lds[threadIdx.x / LANES][(i * LANES + lane) * V + e] = d[i][e];
+                for (int e = 0; e < V; ++e) lds[threadIdx.x / LANES * (NA * V * LANES) + (i * LANES + lane) * V + e] = d[i][e];
             __syncthreads();
             for (int c = threadIdx.x; c < hidden; c += THREADS) {
                 float v = 0.f;
 #pragma unroll
-                for (int g = 0; g < ROWS; ++g) v += lds[g][c];
+                for (int g = 0; g < ROWS; ++g) v += lds[g * (NA * V * LANES) + c];
                 out[c] = v;
             }
         } else {
@@ -248,53 +272,92 @@ __global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(c
     }
 }
 
-// dw[c] += sum over the n rows of partial sums, (db: the same, behind them).  64 columns and 16 waves a workgroup.
+template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
+__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
+                                                                               float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
+{
+    __shared__ float red[2][LAYER ? 2 : 1][16];
+    __shared__ float lds[LANES < 256 ? NA * (16 / sizeof(T)) * 256 : 1];
+    norm_bwd<T, LANES, NA, LAYER, WHOLE>(S, W, stats, dY, dR, dX, partial, rows, hidden, want_w, want_b, red, lds);
+}
+
+// dw[c] += sum over the n rows of partial sums (db: the same, behind them).  32 columns (a cache line) and 32 shares of the
+// rows a workgroup.
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, int n, int hidden, float* d0, float* d1)
 {
-    __shared__ float part[16][64];
-    const int lane = threadIdx.x % 64, w = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    constexpr int COLS = 32, SHARES = 1024 / COLS, U = 8;
+    __shared__ float part[SHARES][COLS];
+    const int lane = threadIdx.x % COLS, w = threadIdx.x / COLS, c = blockIdx.x * COLS + lane;
     const float* p = partial + (int64_t)blockIdx.y * n * hidden + c;
     float v = 0.f;
-    if (c < hidden)
-        for (int r = w; r < n; r += 16) v += p[(int64_t)r * hidden];
+    if (c < hidden) {
+        int r = w;
+        for (; r + (U - 1) * SHARES < n; r += U * SHARES) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = p[(int64_t)(r + u * SHARES) * hidden];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v += x[u];
+        }
+        for (; r < n; r += SHARES) v += p[(int64_t)r * hidden];
+    }
     part[w][lane] = v;
     __syncthreads();
     if (w || c >= hidden) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += part[i][lane];
+    for (int i = 1; i < SHARES; ++i) v += part[i][lane];
     float* d = blockIdx.y == 0 ? d0 : d1;
     d[c] += v;
 }
 
 // Rows of partial sums (workgroups of the backward) at most.
-constexpr int BWD_GROUPS = 1024;
+#ifndef GROUPS
+#define GROUPS 1024
+#endif
+constexpr int BWD_GROUPS = GROUPS;
 
-// f(lanes, accesses) as integral constants for a row of n accesses
+#ifndef F256
+#define F256 64, 4
+#define F512 256, 2
+#define F1024 256, 4
+#define B128 64, 2
+#define B512 256, 2
+#define B1024 512, 2
+#endif
+// f(Shape) for a row of n accesses of elements of T
 template <int L, int N> struct Shape {
     static constexpr int lanes = L, accesses = N;
 };
-template <class F> void fwd_shape(int n, F f)
+template <class T, class F> void fwd_shape(int n, F f)
 {
     if (n <= 16) f(Shape<16, 1>());
     else if (n <= 32) f(Shape<16, 2>());
     else if (n <= 64) f(Shape<64, 1>());
     else if (n <= 128) f(Shape<64, 2>());
-    else if (n <= 256) f(Shape<64, 4>());
-    else if (n <= 512) f(Shape<64, 8>());
-    else if (n <= 1024) f(Shape<256, 4>());
-    else if (n <= 2048) f(Shape<256, 8>());
-    else f(Shape<1024, 4>());
+    else if (n <= 256) f(Shape<F256>());
+    else if (n <= 512) f(Shape<F512>());
+    else if (n <= 1024) f(Shape<F1024>());
+    else if (n <= 2048) f(Shape<512, 4>());
+    else if constexpr (sizeof(T) == 4) f(Shape<1024, 4>());
 }
-template <class F> void bwd_shape(int n, F f)
+template <class T, class F> void bwd_shape(int n, F f)
 {
     if (n <= 16) f(Shape<16, 1>());
     else if (n <= 64) f(Shape<64, 1>());
-    else if (n <= 128) f(Shape<64, 2>());
+    else if (n <= 128) f(Shape<B128>());
     else if (n <= 256) f(Shape<256, 1>());
-    else if (n <= 512) f(Shape<256, 2>());
-    else if (n <= 1024) f(Shape<256, 4>());
+    else if (n <= 512) f(Shape<B512>());
+    else if (n <= 1024) f(Shape<B1024>());
     else if (n <= 2048) f(Shape<1024, 2>());
-    else f(Shape<1024, 4>());
+    else if constexpr (sizeof(T) == 4) f(Shape<1024, 4>());
+}
+// f(std::true_type or false_type) for each of two rules
+template <class F> void by_rule(bool a, bool b, F f)
+{
+    if (a && b) f(std::true_type(), std::true_type());
+    else if (a) f(std::true_type(), std::false_type());
+    else if (b) f(std::false_type(), std::true_type());
+    else f(std::false_type(), std::false_type());
 }
 
 int check(int64_t rows, int hidden, int kind, int dtype)
@@ -326,13 +389,13 @@ void launch_fwd(const void* X, const void* R, const void* W, const void* B, void
 {
     constexpr int V = 16 / sizeof(T);
     auto t = [](const void* p) { return static_cast<const T*>(p); };
-    fwd_shape((hidden + V - 1) / V, [&](auto shape) {
+    fwd_shape<T>((hidden + V - 1) / V, [&](auto shape) {
         constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
         const unsigned grid = groups_of(rows, THREADS / L, 1 << 22);
-        if (kind == FPDT_TW_LAYERNORM)
-            norm_fwd_kernel<T, L, N, true><<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
-        else
-            norm_fwd_kernel<T, L, N, false><<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), nullptr, static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+        by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
+            norm_fwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
+                <<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+        });
     });
 }
 
@@ -342,15 +405,15 @@ void launch_bwd(const void* S, const void* W, const float* stats, const void* dY
 {
     constexpr int V = 16 / sizeof(T);
     auto t = [](const void* p) { return static_cast<const T*>(p); };
-    bwd_shape((hidden + V - 1) / V, [&](auto shape) {
+    bwd_shape<T>((hidden + V - 1) / V, [&](auto shape) {
         constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
         const unsigned grid = groups_of(rows, THREADS / L, BWD_GROUPS);
-        if (kind == FPDT_TW_LAYERNORM)
-            norm_bwd_kernel<T, L, N, true><<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
-        else
-            norm_bwd_kernel<T, L, N, false><<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, false);
+        by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
+            norm_bwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
+                <<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
+        });
         if (dW || dB)
-            norm_sums_kernel<<<dim3((hidden + 63) / 64, dW && dB ? 2 : 1), 1024, 0, st>>>(partial, (int)grid, hidden, dW ? dW : dB, dB);
+            norm_sums_kernel<<<dim3((hidden + 31) / 32, dW && dB ? 2 : 1), 1024, 0, st>>>(partial, (int)grid, hidden, dW ? dW : dB, dB);
     });
 }
 
