@@ -104,11 +104,34 @@ template <int V> __device__ __forceinline__ Vec<uint16_t, V> rounded(const float
     return v;
 }
 
-// Sum over `lanes` consecutive lanes (a power of two), in every one of them.
-template <int LANES, class F> __device__ __forceinline__ F lanes_sum(F v)
+template <int N> struct Int {
+    static constexpr int value = N;
+};
+
+// Sum over LANES consecutive lanes (16, 32 or 64, from a multiple of them on), in every one of them: rotations by 8, 4, 2 and 1 of 16
+// lanes, then with the other rows of 16.  All lanes of the rows have to be active.
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
+{
+    static_assert(LANES == 16 || LANES == 32 || LANES == 64, "");
+    auto turned = [](float x, auto by) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };
+    v += turned(v, Int<8>());
+    v += turned(v, Int<4>());
+    v += turned(v, Int<2>());
+    v += turned(v, Int<1>());
+    if constexpr (LANES >= 32) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    if constexpr (LANES == 64) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    return v;
+}
+__device__ __forceinline__ double wave_sum_f64(double v)
 {
 #pragma unroll
-    for (int m = LANES / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
     return v;
 }
 

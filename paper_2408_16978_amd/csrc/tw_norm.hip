@@ -17,36 +17,39 @@ using namespace fpdt_tw;
 
 constexpr int MOST_HIDDEN = 16384;
 
-// Sums of N values over the LANES threads (at most a wave: lanes of it; more: whole waves of the workgroup) of a row,
-// in every one of them.  `red` holds two sums of 16 waves, by turns, so that one barrier is enough.
+// A row belongs to LANES = 16, 32 or 64 lanes of a wave, in workgroups of 256 threads, or (LANES = 0) to all threads of a
+// workgroup, any number of waves up to 16, so that few of them are idle whatever the width.
+constexpr int SMALL = 256;
+template <int LANES> __device__ __forceinline__ int row_lanes() { return LANES ? LANES : (int)blockDim.x; }
+template <int LANES> __device__ __forceinline__ int row_lane() { return LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x; }
+template <int LANES> __device__ __forceinline__ int row_of() { return LANES ? threadIdx.x / (LANES ? LANES : 1) : 0; }
+
+// Sums of N values over the threads of a row, in every one of them.  `red` holds the sums of 16 waves, twice and used by
+// turns, so that one barrier is enough.
 template <int LANES, int N> struct RowSum {
     float (*red)[N][16];
     int turn = 0;
-    __device__ void operator()(float (&v)[N])
+    __device__ __forceinline__ void operator()(float (&v)[N])
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[n]);
-        if constexpr (LANES > 64) {
-            constexpr int W = LANES / 64;
-            const int w = threadIdx.x / 64;
+        for (int n = 0; n < N; ++n) v[n] = lanes_sum<LANES ? LANES : 64>(v[n]);
+        if constexpr (LANES == 0) {
+            const int waves = blockDim.x / 64;
             if ((threadIdx.x & 63) == 0)
 #pragma unroll
-                for (int n = 0; n < N; ++n) red[turn][n][w] = v[n];
+                for (int n = 0; n < N; ++n) red[turn][n][threadIdx.x / 64] = v[n];
             __syncthreads();
+            const int w = threadIdx.x & 15;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                v[n] = 0.f;
-#pragma unroll
-                for (int i = 0; i < W; ++i) v[n] += red[turn][n][i];
-            }
+            for (int n = 0; n < N; ++n) v[n] = lanes_sum<16>(w < waves ? red[turn][n][w] : 0.f);
             turn ^= 1;
         }
     }
 };
 
-// Access i of a lane covers columns [c, c + V), c = (i LANES + lane) V.  WHOLE: hidden is a multiple of V; if not, the last
-// access of a row is cut off, and rows begin anywhere in a cache line: what is written then goes through the caches, which put
-// the parts of a line together.
+// Access i of a lane covers columns [c, c + V), c = (i lanes + lane) V.  WHOLE: hidden is a multiple of V; if not, the last
+// access of a row is cut off.  Past the caches in either case, also where rows end within a cache line (through them, 1000
+// columns took 229 us for 198, 1001 280 for 241).
 template <bool WHOLE, int V, class T> __device__ __forceinline__ Vec<T, V> load_cut(const T* p, int c, int hidden)
 {
     if (WHOLE || c + V <= hidden) return load_once<V>(p + c);
@@ -57,10 +60,8 @@ template <bool WHOLE, int V, class T> __device__ __forceinline__ Vec<T, V> load_
 }
 template <bool WHOLE, int V, class T> __device__ __forceinline__ void store_cut(T* p, int c, int hidden, const Vec<T, V>& v)
 {
-    if (WHOLE) {
+    if (WHOLE || c + V <= hidden) {
         store_once(p + c, v);
-    } else if (c + V <= hidden) {
-        store(p + c, v);
     } else {
 #pragma unroll
         for (int e = 0; e < V; ++e)
@@ -84,34 +85,36 @@ template <class T, int V> __device__ __forceinline__ void forget(Vec<T, V>& v)
     __builtin_memcpy(&v, x, sizeof v);
 }
 
+// Rows of NA accesses of V elements a lane.
 template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
-__device__ __forceinline__ void norm_fwd(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats, int64_t rows, int hidden, float eps,
-                                         float (*red)[1][16])
+__global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats, int64_t rows,
+                                                                          int hidden, float eps)
 {
-    constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES;
+    constexpr int V = 16 / sizeof(T), ROWS = LANES ? SMALL / (LANES ? LANES : 1) : 1;
+    __shared__ float red[2][1][16];
     RowSum<LANES, 1> sum{red};
-    const int lane = threadIdx.x % LANES;
+    const int lanes = row_lanes<LANES>(), lane = row_lane<LANES>();
     const float inv = 1.f / hidden;
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
-        if (row >= rows) break;  // (only where rows are lanes of a wave: no barrier is left out)
+        const int64_t row = r0 + row_of<LANES>(), at = row * hidden;
+        const int width = row < rows ? hidden : 0;  // (lanes without a row take part in the sums)
         Vec<T, V> x[NA], r[NA];
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
+            const int c = (i * lanes + lane) * V;
             x[i] = {};
-            if (c < hidden) x[i] = load_cut<WHOLE, V>(X + at, c, hidden);
+            if (c < width) x[i] = load_cut<WHOLE, V>(X + at, c, hidden);
         }
         if (R) {
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
-                const int c = (i * LANES + lane) * V;
-                if (c < hidden) r[i] = load_cut<WHOLE, V>(R + at, c, hidden);
+                const int c = (i * lanes + lane) * V;
+                if (c < width) r[i] = load_cut<WHOLE, V>(R + at, c, hidden);
             }
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
-                const int c = (i * LANES + lane) * V;
-                if (c >= hidden) continue;
+                const int c = (i * lanes + lane) * V;
+                if (c >= width) continue;
                 float s[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) s[e] = to_float(x[i].e[e]) + to_float(r[i].e[e]);
@@ -132,24 +135,24 @@ __device__ __forceinline__ void norm_fwd(const T* X, const T* R, const T* W, con
         float v[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
-            if (LAYER && WHOLE && c >= hidden) continue;
+            const int c = (i * lanes + lane) * V;
+            if (LAYER && WHOLE && c >= width) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = LAYER && !WHOLE && c + e >= hidden ? 0.f : to_float(x[i].e[e]) - mean;
+                const float d = LAYER && !WHOLE && c + e >= width ? 0.f : to_float(x[i].e[e]) - mean;
                 v[0] = fmaf(d, d, v[0]);
             }
         }
         sum(v);
         const float rstd = 1.f / sqrtf(v[0] * inv + eps);
-        if (stats && lane == 0) {
+        if (stats && lane == 0 && width) {
             if (LAYER) stats[row] = mean;
             stats[(LAYER ? rows : 0) + row] = rstd;
         }
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
-            if (c >= hidden) continue;
+            const int c = (i * lanes + lane) * V;
+            if (c >= width) continue;
             forget(x[i]);
             float y[V];
             const Vec<T, V> w = load_row<WHOLE, V>(W, c, hidden);
@@ -165,59 +168,67 @@ __device__ __forceinline__ void norm_fwd(const T* X, const T* R, const T* W, con
     }
 }
 
-// Rows of LANES threads, NA accesses of V elements each; max(LANES, 256) threads.
-template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
-__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats,
-                                                                               int64_t rows, int hidden, float eps)
+// Waves on a SIMD that the backward's registers are held to, and workgroups on the whole chip by that: one more than fit at
+// once would walk its rows when the others are done.  64K x 4096 in bf16 (8 waves a row): 768 workgroups 373 us, 512 and 1024 of
+// them 436 and 439.
+constexpr int bwd_waves(int accesses) { return accesses == 1 ? 6 : 4; }
+// Rows of partial sums, that is workgroups, at most: 16 MB of them, written and read again.
+constexpr int bwd_most(int hidden) { return hidden <= 2048 ? 2048 : 1024; }
+constexpr int bwd_groups(int threads, int accesses, int hidden)
 {
-    __shared__ float red[2][1][16];
-    norm_fwd<T, LANES, NA, LAYER, WHOLE>(X, R, W, B, S, Y, stats, rows, hidden, eps, red);
+    const int n = 256 * (bwd_waves(accesses) * 4 / (threads / 64));
+    return n < bwd_most(hidden) ? n : bwd_most(hidden);
 }
 
 // Groups of LANES threads walk the rows; a thread keeps its columns' shares of dw and db in registers, a workgroup's
 // groups add theirs up in LDS and leave one row of partial sums each for norm_sums_kernel: no atomics, the same order
 // of sums in every call.
 template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
-__device__ __forceinline__ void norm_bwd(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX, float* partial, int64_t rows, int hidden,
-                                         bool want_w, bool want_b, float (*red)[LAYER ? 2 : 1][16], float* lds)
+__global__ __launch_bounds__((LANES ? SMALL : 1024), bwd_waves(NA)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
+                                                                                         float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
 {
-    constexpr int V = 16 / sizeof(T), THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES, N = LAYER ? 2 : 1;
+    constexpr int V = 16 / sizeof(T), ROWS = LANES ? SMALL / (LANES ? LANES : 1) : 1, N = LAYER ? 2 : 1;
+    __shared__ float red[2][N][16];
+    __shared__ float lds[LANES ? NA * V * SMALL : 1];
     RowSum<LANES, N> sum{red};
-    const int lane = threadIdx.x % LANES;
+    const int lanes = row_lanes<LANES>(), lane = row_lane<LANES>();
     const float inv = 1.f / hidden;
     Vec<T, V> w[NA];
     float dw[NA][V], db[NA][V];
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
-        const int c = (i * LANES + lane) * V;
+        const int c = (i * lanes + lane) * V;
         w[i] = {};
         if (c < hidden) w[i] = load_row<WHOLE, V>(W, c, hidden);
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
     }
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = r0 + threadIdx.x / LANES, at = row * hidden;
-        if (row >= rows) break;
+        const int64_t row = r0 + row_of<LANES>(), at = row * hidden;
+        const int width = row < rows ? hidden : 0;  // (lanes without a row take part in the sums, with zeros)
         Vec<T, V> x[NA], y[NA], r[NA];
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
+            const int c = (i * lanes + lane) * V;
             x[i] = {}, y[i] = {};
-            if (c < hidden) x[i] = load_cut<WHOLE, V>(S + at, c, hidden), y[i] = load_cut<WHOLE, V>(dY + at, c, hidden);
+            if (c < width) x[i] = load_cut<WHOLE, V>(S + at, c, hidden), y[i] = load_cut<WHOLE, V>(dY + at, c, hidden);
         }
         if (dR)
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
-                const int c = (i * LANES + lane) * V;
-                if (c < hidden) r[i] = load_cut<WHOLE, V>(dR + at, c, hidden);
+                const int c = (i * lanes + lane) * V;
+                if (c < width) r[i] = load_cut<WHOLE, V>(dR + at, c, hidden);
             }
-        const float mean = LAYER ? stats[row] : 0.f, rstd = stats[(LAYER ? rows : 0) + row];
+        const float mean = LAYER && width ? stats[row] : 0.f, rstd = width ? stats[(LAYER ? rows : 0) + row] : 0.f;
         float v[N] = {};
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
+            const int c = (i * lanes + lane) * V;
+            if (c >= width) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float dy = to_float(y[i].e[e]);  // (0 behind the row: whatever u is there counts for nothing)
+                if (!WHOLE && c + e >= hidden) continue;
+                const float dy = to_float(y[i].e[e]);
                 const float u = (to_float(x[i].e[e]) - mean) * rstd, h = dy * to_float(w[i].e[e]);
                 v[0] = fmaf(h, u, v[0]);
                 if (LAYER) v[N - 1] += h, db[i][e] += dy;
@@ -228,8 +239,8 @@ __device__ __forceinline__ void norm_bwd(const T* S, const T* W, const float* st
         const float along = v[0] * inv, level = LAYER ? v[N - 1] * inv : 0.f;
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            const int c = (i * LANES + lane) * V;
-            if (c >= hidden) continue;
+            const int c = (i * lanes + lane) * V;
+            if (c >= width) continue;
             forget(x[i]), forget(y[i]), forget(w[i]);
             float d[V];
 #pragma unroll
@@ -247,14 +258,14 @@ __device__ __forceinline__ void norm_bwd(const T* S, const T* W, const float* st
         if (k == 0 ? !want_w : !want_b) continue;
         float* out = partial + ((int64_t)(k == 1 && want_w ? gridDim.x : 0) + blockIdx.x) * hidden;
         float(&d)[NA][V] = k == 0 ? dw : db;
-        if constexpr (ROWS > 1) {
+        if constexpr (LANES) {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < NA; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) lds[threadIdx.x / LANES * (NA * V * LANES) + (i * LANES + lane) * V + e] = d[i][e];
+                for (int e = 0; e < V; ++e) lds[row_of<LANES>() * (NA * V * LANES) + (i * LANES + lane) * V + e] = d[i][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < hidden; c += THREADS) {
+            for (int c = threadIdx.x; c < hidden; c += SMALL) {
                 float v = 0.f;
 #pragma unroll
                 for (int g = 0; g < ROWS; ++g) v += lds[g * (NA * V * LANES) + c];
@@ -265,20 +276,11 @@ __device__ __forceinline__ void norm_bwd(const T* S, const T* W, const float* st
             for (int i = 0; i < NA; ++i)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const int c = (i * LANES + lane) * V + e;
+                    const int c = (i * lanes + lane) * V + e;
                     if (c < hidden) out[c] = d[i][e];
                 }
         }
     }
-}
-
-template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
-__global__ __launch_bounds__((LANES < 256 ? 256 : LANES)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
-                                                                               float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
-{
-    __shared__ float red[2][LAYER ? 2 : 1][16];
-    __shared__ float lds[LANES < 256 ? NA * (16 / sizeof(T)) * 256 : 1];
-    norm_bwd<T, LANES, NA, LAYER, WHOLE>(S, W, stats, dY, dR, dX, partial, rows, hidden, want_w, want_b, red, lds);
 }
 
 // dw[c] += sum over the n rows of partial sums (db: the same, behind them).  32 columns (a cache line) and 32 shares of the
@@ -310,46 +312,29 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, i
     d[c] += v;
 }
 
-// Rows of partial sums (workgroups of the backward) at most.
-#ifndef GROUPS
-#define GROUPS 1024
-#endif
-constexpr int BWD_GROUPS = GROUPS;
-
-#ifndef F256
-#define F256 64, 4
-#define F512 256, 2
-#define F1024 256, 4
-#define B128 64, 2
-#define B512 256, 2
-#define B1024 512, 2
-#endif
-// f(Shape) for a row of n accesses of elements of T
+// f(Shape, threads) for a row of n accesses of elements of T
 template <int L, int N> struct Shape {
     static constexpr int lanes = L, accesses = N;
 };
+template <int N, class F> void wide(int n, F f) { f(Shape<0, N>(), 64 * ((n + 64 * N - 1) / (64 * N))); }
 template <class T, class F> void fwd_shape(int n, F f)
 {
-    if (n <= 16) f(Shape<16, 1>());
-    else if (n <= 32) f(Shape<16, 2>());
-    else if (n <= 64) f(Shape<64, 1>());
-    else if (n <= 128) f(Shape<64, 2>());
-    else if (n <= 256) f(Shape<F256>());
-    else if (n <= 512) f(Shape<F512>());
-    else if (n <= 1024) f(Shape<F1024>());
-    else if (n <= 2048) f(Shape<512, 4>());
-    else if constexpr (sizeof(T) == 4) f(Shape<1024, 4>());
+    if (n <= 16) f(Shape<16, 1>(), SMALL);
+    else if (n <= 32) f(Shape<32, 1>(), SMALL);
+    else if (n <= 64) f(Shape<64, 1>(), SMALL);
+    else if (n <= 512) wide<1>(n, f);
+    else if (n <= 2048) wide<2>(n, f);
+    else if constexpr (sizeof(T) == 4) wide<4>(n, f);
 }
 template <class T, class F> void bwd_shape(int n, F f)
 {
-    if (n <= 16) f(Shape<16, 1>());
-    else if (n <= 64) f(Shape<64, 1>());
-    else if (n <= 128) f(Shape<B128>());
-    else if (n <= 256) f(Shape<256, 1>());
-    else if (n <= 512) f(Shape<B512>());
-    else if (n <= 1024) f(Shape<B1024>());
-    else if (n <= 2048) f(Shape<1024, 2>());
-    else if constexpr (sizeof(T) == 4) f(Shape<1024, 4>());
+    if (n <= 16) f(Shape<16, 1>(), SMALL);
+    else if (n <= 32) f(Shape<32, 1>(), SMALL);
+    else if (n <= 64) f(Shape<32, 2>(), SMALL);
+    else if (n <= 128) f(Shape<64, 2>(), SMALL);
+    else if (n <= 768) wide<1>(n, f);
+    else if (n <= 2048) wide<2>(n, f);
+    else if constexpr (sizeof(T) == 4) wide<4>(n, f);
 }
 // f(std::true_type or false_type) for each of two rules
 template <class F> void by_rule(bool a, bool b, F f)
@@ -389,12 +374,12 @@ void launch_fwd(const void* X, const void* R, const void* W, const void* B, void
 {
     constexpr int V = 16 / sizeof(T);
     auto t = [](const void* p) { return static_cast<const T*>(p); };
-    fwd_shape<T>((hidden + V - 1) / V, [&](auto shape) {
-        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
-        const unsigned grid = groups_of(rows, THREADS / L, 1 << 22);
+    fwd_shape<T>((hidden + V - 1) / V, [&](auto shape, int threads) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses;
+        const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, 1 << 21);
         by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
             norm_fwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
-                <<<grid, THREADS, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+                <<<grid, threads, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
         });
     });
 }
@@ -405,12 +390,12 @@ void launch_bwd(const void* S, const void* W, const float* stats, const void* dY
 {
     constexpr int V = 16 / sizeof(T);
     auto t = [](const void* p) { return static_cast<const T*>(p); };
-    bwd_shape<T>((hidden + V - 1) / V, [&](auto shape) {
-        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses, THREADS = L < 256 ? 256 : L;
-        const unsigned grid = groups_of(rows, THREADS / L, BWD_GROUPS);
+    bwd_shape<T>((hidden + V - 1) / V, [&](auto shape, int threads) {
+        constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses;
+        const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, bwd_groups(threads, N, hidden));
         by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
             norm_bwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
-                <<<grid, THREADS, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
+                <<<grid, threads, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
         });
         if (dW || dB)
             norm_sums_kernel<<<dim3((hidden + 31) / 32, dW && dB ? 2 : 1), 1024, 0, st>>>(partial, (int)grid, hidden, dW ? dW : dB, dB);
@@ -456,7 +441,7 @@ size_t fpdt_tw_norm_bwd_workspace_bytes(int64_t rows, int hidden, int kind)
 {
     if (rows <= 0 || hidden <= 0 || hidden > MOST_HIDDEN || rows > INT32_MAX || (kind != FPDT_TW_RMSNORM && kind != FPDT_TW_LAYERNORM)) return 0;
     // one row of partial sums per workgroup, and never more workgroups than rows
-    return (size_t)groups_of(rows, 1, BWD_GROUPS) * hidden * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
+    return (size_t)groups_of(rows, 1, bwd_most(hidden)) * hidden * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
 }
 
 int fpdt_tw_norm_bwd(const void* S, const void* W, const float* stats, const void* dY, const void* dR, void* dX, float* dW, float* dB, int64_t rows,

@@ -70,7 +70,7 @@ struct NormArgs {
 
 __device__ double group_sum(double v, double* lds)
 {
-    v = lanes_sum<64>(v);
+    v = wave_sum_f64(v);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
     v = 0;

@@ -88,7 +88,7 @@ template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) vo
                     for (int u = 0; u < U; ++u)
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (h + u < to && (c == 0 || turns)) x[u][c] = load<V>(in + (int64_t)(h + u) * a.D + at[c]);
+                            if (h + u < to && (c == 0 || turns)) x[u][c] = load_once<V>(in + (int64_t)(h + u) * a.D + at[c]);
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         if (h + u >= to) break;
@@ -106,7 +106,7 @@ template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) vo
                         }
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (c == 0 || turns) store(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
+                            if (c == 0 || turns) store_once(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
                     }
                 }
             }
