@@ -4,8 +4,8 @@
 // the same with -t.  Every element is read once and written once: bound by the memory.
 //
 // The angle is formed in 64 bits (at 2M tokens a 32-bit product is off by 0.1 rad), turned into turns and reduced to an
-// eighth of a turn there; sine and cosine of what is left are polynomials in 32 bits.  That is about 30 instructions a
-// pair, so a thread keeps its pairs' sines and cosines for all heads of its token: no table is read.
+// eighth of a turn there; sine and cosine of what is left are polynomials in 32 bits.  That is about 50 instructions a
+// pair, so a thread keeps its pairs' sines and cosines for all heads of its token: no table is read from memory.
 #include <cmath>
 
 #include "../../include/fpdt_tokenwise.h"
@@ -14,6 +14,15 @@
 namespace {
 
 using namespace fpdt_tw;
+
+// What a wave of rope_any_kernel handles at a time of a tensor: `heads` heads of each of `tokens` tokens; per_token units to get
+// through a token's heads (then tokens is 1).  by_*: 2^16 or 2^32 over a divisor, rounded up, in place of a quotient of numbers below 2^9,
+// or of units.
+struct Unit {
+    int tokens, heads, per_token;
+    int by_heads, by_tokens;
+    unsigned by_units;
+};
 
 struct RopeArgs {
     const void* in[3];   // Q, K, V
@@ -27,6 +36,8 @@ struct RopeArgs {
     int D, rot;
     int slots, tokens;  // slots of a head, tokens of a workgroup
     int split;          // heads of a workgroup (of all three tensors together)
+    int by_access, by_pairs;
+    Unit unit[3];
 };
 
 // sin and cos of 2 pi x, times `amplitude`.  x is reduced to within 1/8 of a multiple of 1/4 in 64 bits; the remainders of
@@ -46,13 +57,20 @@ __device__ __forceinline__ void sincos_turns(double x, float amplitude, float& s
 
 // A slot of a head: V pairs in two accesses of V elements (halves; both layouts at V = 1), V / 2 pairs in one access
 // (interleaved, V > 1), and behind the rotated channels V elements that are copied.
-template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
+// LINES: what neighbouring lanes access are whole cache lines, which then go past the caches (65536 tokens, 8 / 2 heads of 128 in bf16 71 us
+// for 79, interleaved 32 / 8 289 for 311; where they are not, 4 / 4 heads of 80 226 for 185).
+template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
 {
     constexpr bool ONE = INTERLEAVED && V > 1;
     constexpr int PAIRS = ONE ? V / 2 : V, ACC = ONE ? 1 : 2, U = 4;
     const int turning = ONE ? a.rot / V : a.rot / 2 / V;
     const int lane = threadIdx.x / a.slots;  // token of the workgroup
     const int h0 = blockIdx.y * a.split;
+    auto get = [](const T* p) { return LINES ? load_once<V>(p) : load<V>(p); };
+    auto put = [](T* p, const Vec<T, V>& v) {
+        if (LINES) store_once(p, v);
+        else store(p, v);
+    };
     for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.rows; t0 += (int64_t)gridDim.x * a.tokens) {
         const int64_t row = t0 + lane;
         if (lane >= a.tokens || row >= a.rows) continue;
@@ -88,7 +106,7 @@ template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) vo
                     for (int u = 0; u < U; ++u)
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (h + u < to && (c == 0 || turns)) x[u][c] = load_once<V>(in + (int64_t)(h + u) * a.D + at[c]);
+                            if (h + u < to && (c == 0 || turns)) x[u][c] = get(in + (int64_t)(h + u) * a.D + at[c]);
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         if (h + u >= to) break;
@@ -106,7 +124,7 @@ template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) vo
                         }
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (c == 0 || turns) store_once(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
+                            if (c == 0 || turns) put(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
                     }
                 }
             }
@@ -114,12 +132,170 @@ template <class T, int V, bool INTERLEAVED> __global__ __launch_bounds__(256) vo
     }
 }
 
+// Where 16 bytes do not fit the pairs (half of rot is odd, or twice an odd number): a workgroup turns `tokens` tokens.  A head is A = D / V accesses
+// in neighbouring lanes, and a wave's 64 / A heads lie one behind the other in memory (those of one token, or of several
+// where these have fewer).  Which token and which heads come next is the same for the wave; a lane's place among them never changes.
+// Partners at a distance come through LDS; sines and cosines of the tile are formed once, in LDS, under the first loads.  65536 tokens, 8 / 2 heads of
+// 128, rot = 30 in halves: 78 us, 182 with slots of one element; with slots of four (heads of 80, rot = 40) these are as fast, 122 us for 130.
+constexpr int TABLE = 2048;  // pairs of a tile: 16 KB
+// What lanes of a wave leave in LDS for each other.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <class T, bool INTERLEAVED> __global__ __launch_bounds__(256) void rope_any_kernel(RopeArgs a)
+{
+    constexpr int V = 16 / sizeof(T), U = 4;
+    typedef Vec<T, V> Access;
+    __shared__ float2 table[TABLE];  // cosine and sine
+    __shared__ uintx4 tile[INTERLEAVED ? 1 : 256];
+    const int A = a.D / V, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int sub = lane * a.by_access >> 16, acc = lane - sub * A;  // head of the wave's, access of the head
+    const int half = a.rot / 2;
+
+    // a lane's place in a unit of each tensor: token, head, and where it reads and writes
+    int dtoken[3], dhead[3], lane_in[3], lane_out[3];
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+        dtoken[t] = a.unit[t].tokens > 1 ? sub * a.unit[t].by_heads >> 16 : 0;
+        dhead[t] = sub - dtoken[t] * a.heads[t];
+        lane_in[t] = dtoken[t] * (int)a.in_row[t] + dhead[t] * a.D + acc * V;
+        lane_out[t] = dtoken[t] * (int)a.out_row[t] + dhead[t] * a.D + acc * V;
+        if (sub >= a.unit[t].tokens * a.unit[t].heads) dhead[t] = 1 << 20;  // no place: no head
+    }
+    auto pick = [](int t, auto x, auto y, auto z) { return t == 0 ? x : t == 1 ? y : z; };
+    const T *in0 = static_cast<const T*>(a.in[0]), *in1 = static_cast<const T*>(a.in[1]), *in2 = static_cast<const T*>(a.in[2]);
+    T *out0 = static_cast<T*>(a.out[0]), *out1 = static_cast<T*>(a.out[1]), *out2 = static_cast<T*>(a.out[2]);
+    const int in_row0 = (int)a.in_row[0], in_row1 = (int)a.in_row[1], in_row2 = (int)a.in_row[2];
+    const int out_row0 = (int)a.out_row[0], out_row1 = (int)a.out_row[1], out_row2 = (int)a.out_row[2];
+    const Unit n0 = a.unit[0], n1 = a.unit[1], n2 = a.unit[2];
+    for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.rows; t0 += (int64_t)gridDim.x * a.tokens) {
+        const int tokens = (int)min((int64_t)a.tokens, a.rows - t0);
+        // units of the tile, tensor by tensor
+        const int end0 = ((tokens + n0.tokens - 1) * n0.by_tokens >> 16) * n0.per_token;
+        const int end1 = end0 + ((tokens + n1.tokens - 1) * n1.by_tokens >> 16) * n1.per_token;
+        const int n = end1 + ((tokens + n2.tokens - 1) * n2.by_tokens >> 16) * n2.per_token;
+        Access x[U];
+        bool here[U];
+        int tensor[U], token[U], head[U];  // of the unit
+        auto fetch = [&](int unit0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int unit = unit0 + u * 4 + wave, t = unit < end0 ? 0 : unit < end1 ? 1 : 2;
+                const int k = unit - pick(t, 0, end0, end1), per = pick(t, n0.per_token, n1.per_token, n2.per_token);
+                const int row = per == 1 ? k : (int)__umulhi(k, pick(t, n0.by_units, n1.by_units, n2.by_units));
+                tensor[u] = t, token[u] = row * pick(t, n0.tokens, n1.tokens, n2.tokens), head[u] = (k - row * per) * pick(t, n0.heads, n1.heads, n2.heads);
+                here[u] = unit < n && token[u] + pick(t, dtoken[0], dtoken[1], dtoken[2]) < tokens
+                    && head[u] + pick(t, dhead[0], dhead[1], dhead[2]) < pick(t, a.heads[0], a.heads[1], a.heads[2]);
+                const int64_t row_in = pick(t, in_row0, in_row1, in_row2);
+                const T* in = pick(t, in0, in1, in2) + (t0 + token[u]) * row_in + head[u] * a.D;
+                if (here[u]) x[u] = load_once<V>(in + (unsigned)pick(t, lane_in[0], lane_in[1], lane_in[2]));
+            }
+        };
+        fetch(0);
+        const int wide = 256 * a.by_pairs >> 16;  // tokens at once: a thread keeps its pair
+        const int tk = threadIdx.x * a.by_pairs >> 16, p = threadIdx.x - tk * half;
+        if (tk < wide) {
+            const double f = a.freqs[p] * 0.15915494309189533577;
+            for (int k = tk; k < tokens; k += wide) {
+                const int64_t pos = a.positions ? a.positions[t0 + k] : a.position0 + t0 + k;
+                float sn, cs;
+                sincos_turns((double)pos * f, a.amplitude, sn, cs);
+                table[k * half + p] = make_float2(cs, a.sign * sn);
+            }
+        }
+        __syncthreads();
+        for (int unit0 = 0; unit0 < n; unit0 += 4 * U) {
+            if (unit0) fetch(unit0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (unit0 + u * 4 + wave >= n) continue;
+                const int t = tensor[u];
+                if (t < 2) {
+                    // (lanes without a place read what another token has, and write nothing)
+                    const float2* tab = table + (here[u] ? token[u] + (t == 0 ? dtoken[0] : dtoken[1]) : 0) * half;
+                    float y[V];
+                    if constexpr (INTERLEAVED) {
+#pragma unroll
+                        for (int e = 0; e < V; e += 2) {
+                            const int c = acc * V + e;
+                            y[e] = to_float(x[u].e[e]), y[e + 1] = to_float(x[u].e[e + 1]);
+                            if (here[u] && c < a.rot) {
+                                const float2 k = tab[c / 2];
+                                const float p = y[e], q = y[e + 1];
+                                y[e] = fmaf(p, k.x, -q * k.y), y[e + 1] = fmaf(q, k.x, p * k.y);
+                            }
+                        }
+                    } else {
+                        tile[threadIdx.x] = __builtin_bit_cast(uintx4, x[u]);
+                        wave_sync();
+                        const T* from = reinterpret_cast<const T*>(tile + threadIdx.x - acc);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const int c = acc * V + e;
+                            y[e] = to_float(x[u].e[e]);
+                            if (here[u] && c < a.rot) {
+                                const int i = c < half ? c : c - half;
+                                const float2 k = tab[i];
+                                const float other = to_float(from[c < half ? c + half : i]);
+                                y[e] = fmaf(y[e], k.x, c < half ? -other * k.y : other * k.y);
+                            }
+                        }
+                        wave_sync();
+                    }
+                    x[u] = rounded<V>(y, T());
+                }
+                const int64_t row_out = pick(t, out_row0, out_row1, out_row2);
+                T* out = pick(t, out0, out1, out2) + (t0 + token[u]) * row_out + head[u] * a.D;
+                if (here[u]) store_once(out + (unsigned)pick(t, lane_out[0], lane_out[1], lane_out[2]), x[u]);
+            }
+        }
+        __syncthreads();  // the next tile's table
+    }
+}
+
 constexpr int MOST_D = 8192, MOST_HEADS = 4096;
 
-template <class T, int V> void launch_v(const RopeArgs& a, bool interleaved, dim3 grid, hipStream_t st)
+// Two workgroups on a compute unit, by LDS that nobody uses, from 12 heads on: more of them push each other's lines out of the
+// caches between two accesses to a line (us with all | two, bf16: 256K tokens, 4 / 4 heads of 80, rot = 80 in halves 218 | 196, 32 interleaved 191 | 180,
+// 8 / 2 of 64 159 | 153, 64K, 32 / 8 of 128 interleaved 290 | 280; with fewer heads too little is in flight: 8 / 1 of 128, rot = 64 66 | 71, 1 / 1 of 128 73 | 88).
+template <class T, int V> void launch_v(const RopeArgs& a, bool interleaved, bool lines, dim3 grid, hipStream_t st)
 {
-    if (interleaved) rope_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-    else rope_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+    const size_t lds = a.heads[0] + a.heads[1] + a.heads[2] >= 12 ? 65536 : 0;
+    if constexpr (V * sizeof(T) == 16) {
+        if (lines && interleaved) rope_kernel<T, V, true, true><<<grid, 256, lds, st>>>(a);
+        else if (lines) rope_kernel<T, V, false, true><<<grid, 256, lds, st>>>(a);
+        if (lines) return;
+    }
+    if (interleaved) rope_kernel<T, V, true, false><<<grid, 256, lds, st>>>(a);
+    else rope_kernel<T, V, false, false><<<grid, 256, lds, st>>>(a);
+}
+
+template <class T> void launch_any(RopeArgs& a, bool interleaved, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int per_wave = 64 / (a.D / V);
+    auto by = [](int d) { return (65536 + d - 1) / d; };
+    a.by_access = by(a.D / V), a.by_pairs = by(a.rot / 2);
+    for (int t = 0; t < 3; ++t) {
+        const int h = a.heads[t];
+        Unit& n = a.unit[t];
+        n.tokens = h && h < per_wave ? per_wave / h : 1;
+        n.heads = h < per_wave ? h : per_wave;
+        n.per_token = (h + per_wave - 1) / per_wave;
+        n.by_heads = h ? by(h) : 0, n.by_tokens = by(n.tokens);
+        n.by_units = n.per_token > 1 ? (unsigned)((0x100000000ull + n.per_token - 1) / n.per_token) : 0;
+    }
+    // Tokens of a tile: as many as 16 KB of sines and cosines are, 16 at most, and fewer until there are four workgroups for
+    // each compute unit.
+    a.tokens = TABLE / (a.rot / 2) < 16 ? TABLE / (a.rot / 2) : 16;
+    while (a.tokens > 1 && a.rows / a.tokens < 1024) a.tokens = (a.tokens + 1) / 2;
+    const int64_t tiles = (a.rows + a.tokens - 1) / a.tokens;
+    const unsigned grid = (unsigned)(tiles < (1 << 20) ? tiles : 1 << 20);
+    if (interleaved) rope_any_kernel<T, true><<<grid, 256, 0, st>>>(a);
+    else rope_any_kernel<T, false><<<grid, 256, 0, st>>>(a);
 }
 
 // The widest access whose elements are all turned or all copied, in either half.
@@ -183,25 +359,37 @@ int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], c
     a.positions = positions, a.position0 = position0, a.rows = rows, a.freqs = freqs, a.amplitude = amplitude, a.sign = back ? -1.f : 1.f;
     a.D = D, a.rot = rot;
     const bool inter = layout == FPDT_TW_ROPE_INTERLEAVED;
-    const int v = access(D, rot, inter, 16 / size), heads = a.heads[0] + a.heads[1] + a.heads[2];
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int full = 16 / size, v = access(D, rot, inter, full), heads = a.heads[0] + a.heads[1] + a.heads[2];
+    bool near = true;  // a tile's offsets fit 32 bits
+    for (int t = 0; t < 3; ++t) near = near && in_row[t] <= (1 << 24) && out_row[t] <= (1 << 24);
+    if (v <= full / 4 && D % full == 0 && D / full <= 64 && near) {
+        if (size == 4) launch_any<float>(a, inter, st);
+        else launch_any<uint16_t>(a, inter, st);
+        HIP_TRY(hipGetLastError());
+        return TW_OK;
+    }
     a.slots = (inter && v > 1 ? rot / v : rot / 2 / v) + (D - rot) / v;
     a.tokens = a.slots >= 256 ? 1 : 256 / a.slots;
+    // What the lanes of a token access: a head (interleaved), or a half and what is copied.
+    bool lines = v == full && D * size % 128 == 0 && (inter || rot / 2 * size % 128 == 0);
+    for (int t = 0; t < 3; ++t)
+        lines = lines && !misaligned(a.in[t], 128) && !misaligned(a.out[t], 128) && a.in_row[t] * size % 128 == 0 && a.out_row[t] * size % 128 == 0;
     const int64_t tiles = (rows + a.tokens - 1) / a.tokens;
     // All heads of a token in one thread, as long as that leaves every compute unit some workgroups.
     int parts = tiles >= 1024 ? 1 : (int)((1024 + tiles - 1) / tiles);
     if (parts > heads) parts = heads;
     a.split = (heads + parts - 1) / parts;
     const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((heads + a.split - 1) / a.split));
-    hipStream_t st = static_cast<hipStream_t>(stream);
     if (size == 4) {
-        if (v == 4) launch_v<float, 4>(a, inter, grid, st);
-        else if (v == 2) launch_v<float, 2>(a, inter, grid, st);
-        else launch_v<float, 1>(a, inter, grid, st);
+        if (v == 4) launch_v<float, 4>(a, inter, lines, grid, st);
+        else if (v == 2) launch_v<float, 2>(a, inter, lines, grid, st);
+        else launch_v<float, 1>(a, inter, lines, grid, st);
     } else {
-        if (v == 8) launch_v<uint16_t, 8>(a, inter, grid, st);
-        else if (v == 4) launch_v<uint16_t, 4>(a, inter, grid, st);
-        else if (v == 2) launch_v<uint16_t, 2>(a, inter, grid, st);
-        else launch_v<uint16_t, 1>(a, inter, grid, st);
+        if (v == 8) launch_v<uint16_t, 8>(a, inter, lines, grid, st);
+        else if (v == 4) launch_v<uint16_t, 4>(a, inter, lines, grid, st);
+        else if (v == 2) launch_v<uint16_t, 2>(a, inter, lines, grid, st);
+        else launch_v<uint16_t, 1>(a, inter, lines, grid, st);
     }
     HIP_TRY(hipGetLastError());
     return TW_OK;
