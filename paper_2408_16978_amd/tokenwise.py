@@ -158,18 +158,25 @@ def _dtype_code(t):
 
 
 def _expect(name, t, shape, dtype, device):
-    """`t` is a contiguous tensor of that shape and type on that device."""
-    if t.dtype != dtype or t.device != device:
-        raise TypeError("fpdt_tw: %s must be %s on %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
+    """`t` is a contiguous tensor of that shape and type on that device (an index)."""
+    if t.dtype != dtype or t.get_device() != device:
+        raise TypeError("fpdt_tw: %s must be %s on device %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
     if t.shape != shape or not t.is_contiguous():
         raise ValueError("fpdt_tw: %s must be contiguous and %s, got %s with strides %s" % (name, tuple(shape), tuple(t.shape), t.stride()))
+    return t.data_ptr()
 
 
 def _current(t):
-    """The device of `t`, which has to be the current one: calls go to its stream."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    """The index of `t`'s device, which has to be the current one: calls go to its stream."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
         raise ValueError("fpdt_tw: tensors must be on the current device, got %s" % t.device)
-    return t.device
+    return device
+
+
+def _raw_stream(stream, device):
+    # (a stream object of torch's costs as much to make as the rest of a small call)
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def fpdt_tw_rope_freqs(rot, base, scaling=FPDT_TW_ROPE_PLAIN, factor=1.0, context=0.0, low=1.0, high=4.0):
@@ -185,26 +192,25 @@ def _rope(call, ins, outs, freqs, positions, position0, amplitude, layout, strea
     if Q.dim() != 3:
         raise ValueError("fpdt_tw: Q must be [rows, heads, D], got %s" % (tuple(Q.shape),))
     rows, Hq, D = Q.shape
-    Hkv = 0 if ins[1] is None and ins[2] is None else (ins[1] if ins[1] is not None else ins[2]).shape[1]
+    other = ins[1] if ins[1] is not None else ins[2]
+    Hkv = 0 if other is None else other.size(1)
     args = []
-    for name, heads, pair in zip("QKV", (Hq, Hkv, Hkv), zip(ins, outs)):
-        if (pair[0] is None) != (pair[1] is None):
-            raise ValueError("fpdt_tw: %s is given on one side only" % name)
-    for side in (ins, outs):
-        for name, heads, t in zip("QKV", (Hq, Hkv, Hkv), side):
-            if t is None:
-                args += [None, 0]
-                continue
-            if t.dtype != dtype or t.device != device:
-                raise TypeError("fpdt_tw: %s must be %s on %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
-            if t.shape != (rows, heads, D) or (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
-                raise ValueError("fpdt_tw: %s must be %s with contiguous heads, got %s with strides %s" % (
-                    name, (rows, heads, D), tuple(t.shape), t.stride()))
-            args += [t.data_ptr(), t.stride(0) if rows > 1 else heads * D]
-    _expect("freqs", freqs, freqs.shape[:1], torch.float64, device)
-    if positions is not None:
-        _expect("positions", positions, (rows,), torch.int64, device)
-    _check(call(*args, _ptr(positions), position0, freqs.data_ptr(), amplitude, rows, Hq, Hkv, D, 2 * freqs.numel(), layout, code, _stream(stream)))
+    for name, heads, t, o in zip("QKVQKV", (Hq, Hkv, Hkv) * 2, ins + outs, outs + ins):
+        if t is None:
+            if o is not None:
+                raise ValueError("fpdt_tw: %s is given on one side only" % name)
+            args += (None, 0)
+            continue
+        if t.dtype != dtype or t.get_device() != device:
+            raise TypeError("fpdt_tw: %s must be %s on device %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
+        strides = t.stride()
+        if t.shape != (rows, heads, D) or (D > 1 and strides[2] != 1) or (heads > 1 and strides[1] != D):
+            raise ValueError("fpdt_tw: %s must be %s with contiguous heads, got %s with strides %s" % (name, (rows, heads, D), tuple(t.shape), strides))
+        args += (t.data_ptr(), strides[0] if rows > 1 else heads * D)
+    half = freqs.numel()
+    args += (None if positions is None else _expect("positions", positions, (rows,), torch.int64, device), position0,
+             _expect("freqs", freqs, (half,), torch.float64, device), amplitude, rows, Hq, Hkv, D, 2 * half, layout, code, _raw_stream(stream, device))
+    _check(call(*args))
 
 
 def fpdt_tw_rope_fwd(Q, K, V, Qo, Ko, Vo, freqs, positions=None, position0=0, amplitude=1.0, layout=FPDT_TW_ROPE_HALF, stream=None):
@@ -221,19 +227,20 @@ def fpdt_tw_rope_bwd(dQo, dKo, dVo, dQ, dK, dV, freqs, positions=None, position0
 def fpdt_tw_norm_fwd(X, R, W, B, S, Y, stats, eps, kind=FPDT_TW_RMSNORM, stream=None):
     """S = X + R (R and S, or S, may be None), Y = normalised S times W [hidden] (plus B, LAYERNORM).  stats: None, or fp32 of
     rows (RMSNORM: rstd) or 2 rows (LAYERNORM: mean, rstd) values for the backward."""
-    device, code = _current(X), _dtype_code(X)
+    device, dtype, code = _current(X), X.dtype, _dtype_code(X)
     rows, hidden = X.shape
-    for name, t, shape in (("X", X, X.shape), ("R", R, X.shape), ("S", S, X.shape), ("Y", Y, X.shape), ("W", W, (hidden,)), ("B", B, (hidden,))):
-        if t is not None:
-            _expect(name, t, shape, X.dtype, device)
-    _expect_stats(stats, rows, kind, device)
-    _check(load().fpdt_tw_norm_fwd(_ptr(X), _ptr(R), _ptr(W), _ptr(B), _ptr(S), _ptr(Y), _ptr(stats), rows, hidden, kind, eps, code, _stream(stream)))
+    at = [None if t is None else _expect(name, t, shape, dtype, device) for name, t, shape in (
+        ("X", X, X.shape), ("R", R, X.shape), ("W", W, (hidden,)), ("B", B, (hidden,)), ("S", S, X.shape), ("Y", Y, X.shape))]
+    _check(load().fpdt_tw_norm_fwd(*at, _stats(stats, rows, kind, device), rows, hidden, kind, eps, code, _raw_stream(stream, device)))
 
 
-def _expect_stats(stats, rows, kind, device):
+def _stats(stats, rows, kind, device):
+    if stats is None:
+        return None
     n = rows * (2 if kind == FPDT_TW_LAYERNORM else 1)
-    if stats is not None and (stats.dtype != torch.float32 or stats.device != device or stats.numel() != n or not stats.is_contiguous()):
-        raise ValueError("fpdt_tw: stats must be %d contiguous float32 values on %s" % (n, device))
+    if stats.dtype != torch.float32 or stats.get_device() != device or stats.numel() != n or not stats.is_contiguous():
+        raise ValueError("fpdt_tw: stats must be %d contiguous float32 values on device %s" % (n, device))
+    return stats.data_ptr()
 
 
 def fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind=FPDT_TW_RMSNORM) -> int:
@@ -242,17 +249,13 @@ def fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind=FPDT_TW_RMSNORM) -> int:
 
 def fpdt_tw_norm_bwd(S, W, stats, dY, dR, dX, dW, dB, kind=FPDT_TW_RMSNORM, workspace=None, stream=None):
     """dX (written) = gradient through the norm plus dR (or None); dW, dB fp32 [hidden] (accumulated into, or None)."""
-    device, code = _current(S), _dtype_code(S)
+    device, dtype, code = _current(S), S.dtype, _dtype_code(S)
     rows, hidden = S.shape
-    for name, t, shape in (("S", S, S.shape), ("dY", dY, S.shape), ("dR", dR, S.shape), ("dX", dX, S.shape), ("W", W, (hidden,))):
-        if t is not None:
-            _expect(name, t, shape, S.dtype, device)
-    for name, t in (("dW", dW), ("dB", dB)):
-        if t is not None:
-            _expect(name, t, (hidden,), torch.float32, device)
-    _expect_stats(stats, rows, kind, device)
-    _check(load().fpdt_tw_norm_bwd(_ptr(S), _ptr(W), _ptr(stats), _ptr(dY), _ptr(dR), _ptr(dX), _ptr(dW), _ptr(dB), rows, hidden, kind, code,
-                                   _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    at = [None if t is None else _expect(name, t, shape, dtype, device) for name, t, shape in (
+        ("S", S, S.shape), ("W", W, (hidden,)), ("dY", dY, S.shape), ("dR", dR, S.shape), ("dX", dX, S.shape))]
+    sums = [None if t is None else _expect(name, t, (hidden,), torch.float32, device) for name, t in (("dW", dW), ("dB", dB))]
+    _check(load().fpdt_tw_norm_bwd(at[0], at[1], _stats(stats, rows, kind, device), *at[2:], *sums, rows, hidden, kind, code, _ptr(workspace), _nbytes(workspace),
+                                   _raw_stream(stream, device)))
 
 
 class _Param(ctypes.Structure):
@@ -298,11 +301,12 @@ class FpdtTwParams:
             if b[0] < a[1]:
                 raise ValueError("fpdt_tw: %s and %s overlap" % (a[2], b[2]))
         self._keep = [tensors for tensors, _ in given.values()]
+        self.address = ctypes.addressof(self.array)
 
     def _args(self):
         if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
             raise ValueError("fpdt_tw: tensors must be on the current device, got %s" % self.device)
-        return self.array, self.count
+        return self.address, self.count
 
 
 def fpdt_tw_grad_norm_workspace_bytes(params) -> int:
@@ -311,20 +315,21 @@ def fpdt_tw_grad_norm_workspace_bytes(params) -> int:
 
 def fpdt_tw_grad_norm(params, max_norm, out, workspace, stream=None):
     """out (fp32 [2]): norm of all gradients, and the factor that brings it down to max_norm."""
-    args = params._args()
-    _expect("out", out, (2,), torch.float32, params.device)
-    _check(load().fpdt_tw_grad_norm(*args, params.grad_dtype, max_norm, _ptr(out), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    args, device = params._args(), params.device.index
+    _check(load().fpdt_tw_grad_norm(*args, params.grad_dtype, max_norm, _expect("out", out, (2,), torch.float32, device), _ptr(workspace),
+                                    _nbytes(workspace), _raw_stream(stream, device)))
 
 
 def fpdt_tw_adamw_step(params, lr, beta1, beta2, eps, step, lr_dev=None, step_dev=None, grad_scale=None, seed=0, flags=0, stream=None):
     """One step.  lr_dev (fp32), step_dev (int64), grad_scale (fp32): one value each on the device, or None; lr and step are
     ignored where lr_dev and step_dev are given."""
-    args = params._args()
+    args, device, at = params._args(), params.device.index, []
     for name, t, dtype in (("lr_dev", lr_dev, torch.float32), ("step_dev", step_dev, torch.int64), ("grad_scale", grad_scale, torch.float32)):
-        if t is not None and (t.dtype != dtype or t.device != params.device or t.numel() != 1):
+        if t is not None and (t.dtype != dtype or t.get_device() != device or t.numel() != 1):
             raise ValueError("fpdt_tw: %s must be one %s on %s" % (name, dtype, params.device))
-    _check(load().fpdt_tw_adamw_step(*args, params.grad_dtype, params.state_bits, lr, beta1, beta2, eps, step, _ptr(lr_dev), _ptr(step_dev),
-                                     _ptr(grad_scale), seed & 0xffffffff, flags, _stream(stream)))
+        at.append(None if t is None else t.data_ptr())
+    _check(load().fpdt_tw_adamw_step(*args, params.grad_dtype, params.state_bits, lr, beta1, beta2, eps, step, *at, seed & 0xffffffff, flags,
+                                     _raw_stream(stream, device)))
 
 
 def fpdt_tw_adamw_unpack(params, stream=None):
@@ -332,4 +337,4 @@ def fpdt_tw_adamw_unpack(params, stream=None):
     args = params._args()
     if params.state_bits != 8:
         raise ValueError("fpdt_tw: the list's states are in 32 bits")
-    _check(load().fpdt_tw_adamw_unpack(*args, _stream(stream)))
+    _check(load().fpdt_tw_adamw_unpack(*args, _raw_stream(stream, params.device.index)))
