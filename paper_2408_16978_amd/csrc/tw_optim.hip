@@ -13,10 +13,16 @@ namespace {
 
 using namespace fpdt_tw;
 
-constexpr int UNIT = 4096;        // elements: 16 of each of 256 threads
-constexpr int NORM_UNIT = 16384;  // of the norm, whose threads only read
+// Elements of a unit: as many as a thread can have under way, where that gives every compute unit four workgroups; a quarter of
+// them otherwise (150 tensors of 64 to 65536 elements, 1.4 million in all: three launches of the step 16.3 us for 20.6, the
+// norm's 4.2 for 4.8).
+constexpr int UNIT = 4096, UNIT8 = 2048, SMALL_UNIT = 1024;  // (8-bit states: 1006 us with 2048, 1034 with 4096, which in 32 bits takes 1281 for 1307)
+constexpr int NORM_UNIT = 16384, SMALL_NORM_UNIT = 4096;
+constexpr int ENOUGH = 1024;  // units
 constexpr int BLOCK = 128;        // elements of a block of 8-bit states
-constexpr int MOST_UNITS = 1 << 23;  // of a launch
+constexpr int MOST_UNITS = (1 << 24) - 1;  // of a launch: fewer than 2^32 lanes
+
+constexpr int64_t MOST_ELEMENTS = (int64_t)UNIT8 * MOST_UNITS;  // of a tensor
 
 // ---- lists of tensors as kernel arguments (at most 4 KB)
 template <class Tensor, int N> struct List {
@@ -80,17 +86,17 @@ __device__ double group_sum(double v, double* lds)
 
 // Squares and sums in 64 bits: no gradient that a float holds overflows or vanishes in them.  A workgroup leaves one
 // partial sum, in the same place and of the same units in every call.
-template <class T> __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a)
+template <class T, int U> __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a)
 {
-    constexpr int V = 16 / sizeof(T), N = NORM_UNIT / 256 / V;
+    constexpr int V = 16 / sizeof(T), N = U / 256 / V;
     __shared__ double lds[4];
     double sum = 0;
     for (unsigned u = blockIdx.x; u < a.units; u += gridDim.x) {
         const int k = find(a.list.first, u);
-        const int64_t at = (int64_t)(u - a.list.first[k]) * NORM_UNIT, left = a.list.t[k].n - at;
+        const int64_t at = (int64_t)(u - a.list.first[k]) * U, left = a.list.t[k].n - at;
         const T* g = static_cast<const T*>(a.list.t[k].g) + at;
         Vec<T, V> x[N];
-        if (left >= NORM_UNIT) {
+        if (left >= U) {
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = load_once<V>(g + (i * 256 + threadIdx.x) * V);
         } else {
@@ -199,19 +205,19 @@ __device__ __forceinline__ void update(const Step& s, float g, float& p, float& 
     p = p * s.keep - m * s.rate * __builtin_amdgcn_rcpf(root);
 }
 
-template <class G> __device__ __forceinline__ void zero_grads(G* g, int64_t left)
+template <class G, int U> __device__ __forceinline__ void zero_grads(G* g, int64_t left)
 {
 #pragma unroll
-    for (int i = 0; i < UNIT / 256 / 4; ++i) {
+    for (int i = 0; i < U / 256 / 4; ++i) {
         const int c = (i * 256 + threadIdx.x) * 4;
         if (c < left) store_to<false>(g + c, left - c, Vec<G, 4>{});
     }
 }
 
-template <class G, bool WHOLE>
+template <class G, int U, bool WHOLE>
 __device__ __forceinline__ void adamw_unit(const Step& s, G* g, float* p, float* m, float* v, uint16_t* w, int64_t left, bool zero)
 {
-    constexpr int V = 4, N = UNIT / 256 / V;
+    constexpr int V = 4, N = U / 256 / V;
     Vec<G, V> xg[N];
     Vec<float, V> xp[N], xm[N], xv[N];
 #pragma unroll
@@ -237,21 +243,21 @@ __device__ __forceinline__ void adamw_unit(const Step& s, G* g, float* p, float*
     }
 }
 
-template <class G> __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<Tensor32, TENSORS32> a)
+template <class G, int U> __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<Tensor32, TENSORS32> a)
 {
     const int k = find(a.list.first, blockIdx.x);
     const Tensor32& t = a.list.t[k];
-    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
+    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * U, left = t.n - at;
     const Step s = make_step(a.h, t.decay);
     G* g = static_cast<G*>(t.g) + at;
     if (s.skip) {
-        if (a.h.zero) zero_grads(g, left);
+        if (a.h.zero) zero_grads<G, U>(g, left);
         return;
     }
     float *m = static_cast<float*>(t.m) + at, *v = static_cast<float*>(t.v) + at;
     uint16_t* w = t.w ? t.w + at : nullptr;
-    if (left >= UNIT) adamw_unit<G, true>(s, g, t.p + at, m, v, w, left, a.h.zero);
-    else adamw_unit<G, false>(s, g, t.p + at, m, v, w, left, a.h.zero);
+    if (left >= U) adamw_unit<G, U, true>(s, g, t.p + at, m, v, w, left, a.h.zero);
+    else adamw_unit<G, U, false>(s, g, t.p + at, m, v, w, left, a.h.zero);
 }
 
 // ---- 8-bit states.  A block of 128 has an exponent byte E, that of its largest value rounded up to three fraction bits (at
@@ -313,11 +319,11 @@ __device__ __forceinline__ unsigned encode_v(float x, unsigned base, unsigned ra
 
 // Four elements of a lane at a time, so that every access of a wave is contiguous (with eight, the two halves of a lane's p
 // and g are 32 bytes from the next lane's).
-template <class G, bool WHOLE>
+template <class G, int U, bool WHOLE>
 __device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8_t* m, uint8_t* v, uint8_t* me, uint8_t* ve, uint16_t* w, unsigned at,
                                             unsigned key, int64_t left, bool zero)
 {
-    constexpr int V = 4, N = UNIT / 256 / V;
+    constexpr int V = 4, N = U / 256 / V;
     Vec<G, V> xg[N];
     Vec<float, V> xp[N];
     Vec<uint8_t, V> xm[N], xv[N];
@@ -371,23 +377,23 @@ __device__ __forceinline__ void adamw8_unit(const Step& s, G* g, float* p, uint8
     }
 }
 
-template <class G> __global__ __launch_bounds__(256) void adamw8_kernel(AdamwArgs<Tensor8, TENSORS8> a)
+template <class G, int U> __global__ __launch_bounds__(256) void adamw8_kernel(AdamwArgs<Tensor8, TENSORS8> a)
 {
     const int k = find(a.list.first, blockIdx.x);
     const Tensor8& t = a.list.t[k];
-    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * UNIT, left = t.n - at;
+    const int64_t at = (int64_t)(blockIdx.x - a.list.first[k]) * U, left = t.n - at;
     const Step s = make_step(a.h, t.decay);
     G* g = static_cast<G*>(t.g) + at;
     if (s.skip) {
-        if (a.h.zero) zero_grads(g, left);
+        if (a.h.zero) zero_grads<G, U>(g, left);
         return;
     }
     unsigned key = mix(mix(mix(a.h.seed ^ 0x243F6A88u) ^ (unsigned)s.step * 0x9E3779B1u) ^ t.ordinal * 0x85A308D3u);
     if (at >> 32) key = mix(key + (unsigned)(at >> 32));
     uint8_t *m = static_cast<uint8_t*>(t.m) + at, *v = static_cast<uint8_t*>(t.v) + at, *me = t.m_exp + at / BLOCK, *ve = t.v_exp + at / BLOCK;
     uint16_t* w = t.w ? t.w + at : nullptr;
-    if (left >= UNIT) adamw8_unit<G, true>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
-    else adamw8_unit<G, false>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
+    if (left >= U) adamw8_unit<G, U, true>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
+    else adamw8_unit<G, U, false>(s, g, t.p + at, m, v, me, ve, w, (unsigned)at, key, left, a.h.zero);
 }
 
 struct Unpacked {
@@ -463,13 +469,21 @@ template <class L, int N, class Take, class Launch> int in_launches(const fpdt_t
     return TW_OK;
 }
 
+// Units of a list, in all
+int64_t units_of(const fpdt_tw_param* params, int count, int unit)
+{
+    int64_t n = 0;
+    for (int k = 0; k < count; ++k) n += (params[k].n + unit - 1) / unit;
+    return n;
+}
+
 int check_list(const fpdt_tw_param* params, int count, int grad_dtype)
 {
     if (!params || count <= 0) return fail(TW_INVALID, "params NULL or count not positive");
     if (grad_dtype != FPDT_TW_F32 && grad_dtype != FPDT_TW_BF16) return fail(TW_INVALID, "unknown grad_dtype %d", grad_dtype);
     for (int k = 0; k < count; ++k) {
         if (params[k].n < 0) return fail(TW_INVALID, "tensor %d has %lld elements", k, (long long)params[k].n);
-        if (params[k].n > (int64_t)UNIT * MOST_UNITS) return fail(TW_UNSUPPORTED, "tensor %d: %lld elements are beyond the launch limits", k, (long long)params[k].n);
+        if (params[k].n > MOST_ELEMENTS) return fail(TW_UNSUPPORTED, "tensor %d: %lld elements are beyond the launch limits", k, (long long)params[k].n);
         if (params[k].n && (!params[k].g || misaligned(params[k].g, grad_dtype == FPDT_TW_F32 ? 4 : 2)))
             return fail(TW_INVALID, "tensor %d: g is NULL or not aligned to its elements", k);
     }
@@ -493,9 +507,10 @@ int fpdt_tw_grad_norm(const fpdt_tw_param* params, int count, int grad_dtype, do
     if (rc != TW_OK) return rc;
     if (!out || misaligned(out, 4)) return fail(TW_INVALID, "out is NULL or not aligned to its elements");
     if (!(max_norm > 0)) return fail(TW_INVALID, "max_norm must be positive");
-    int64_t units = 0;  // of one launch's share at most in all: a list needs a launch for each NORM_TENSORS tensors then
-    for (int k = 0; k < count; ++k) units += (params[k].n + NORM_UNIT - 1) / NORM_UNIT;
-    if (units > MOST_UNITS) return fail(TW_UNSUPPORTED, "the list's elements are beyond the launch limits");
+    // (a list needs one launch for each NORM_TENSORS tensors then)
+    const int64_t all = units_of(params, count, NORM_UNIT);
+    const int unit = all >= ENOUGH ? NORM_UNIT : SMALL_NORM_UNIT;
+    if (all > MOST_UNITS) return fail(TW_UNSUPPORTED, "the list's elements are beyond the launch limits");
     const size_t need = fpdt_tw_grad_norm_workspace_bytes(count);
     if (!workspace || workspace_bytes < need || misaligned(workspace, 256))
         return fail(TW_WORKSPACE, "workspace NULL, misaligned or too small (%zu < %zu bytes)", workspace_bytes, need);
@@ -504,13 +519,16 @@ int fpdt_tw_grad_norm(const fpdt_tw_param* params, int count, int grad_dtype, do
     double* partial = static_cast<double*>(workspace);
     int n = 0;
     rc = in_launches<decltype(a.list), NORM_TENSORS>(
-        params, count, NORM_UNIT, a.list, [&](NormTensor& t, int k) { t = {params[k].g, params[k].n}; },
+        params, count, unit, a.list, [&](NormTensor& t, int k) { t = {params[k].g, params[k].n}; },
         [&](unsigned units) {
             const unsigned grid = units < NORM_GROUPS ? units : NORM_GROUPS;
             a.partial = partial + n, a.units = units;
             n += (int)grid;
-            if (grad_dtype == FPDT_TW_F32) grad_norm_kernel<float><<<grid, 256, 0, st>>>(a);
-            else grad_norm_kernel<uint16_t><<<grid, 256, 0, st>>>(a);
+            const bool wide = grad_dtype == FPDT_TW_F32;
+            if (unit == NORM_UNIT && wide) grad_norm_kernel<float, NORM_UNIT><<<grid, 256, 0, st>>>(a);
+            else if (unit == NORM_UNIT) grad_norm_kernel<uint16_t, NORM_UNIT><<<grid, 256, 0, st>>>(a);
+            else if (wide) grad_norm_kernel<float, SMALL_NORM_UNIT><<<grid, 256, 0, st>>>(a);
+            else grad_norm_kernel<uint16_t, SMALL_NORM_UNIT><<<grid, 256, 0, st>>>(a);
         });
     if (rc != TW_OK) return rc;
     grad_norm_end_kernel<<<1, 1024, 0, st>>>(partial, n, max_norm, out);
@@ -551,25 +569,31 @@ int fpdt_tw_adamw_step(const fpdt_tw_param* params, int count, int grad_dtype, i
         const fpdt_tw_param& x = params[k];
         t.p = x.p, t.w = static_cast<uint16_t*>(x.w), t.g = x.g, t.m = x.m, t.v = x.v, t.n = x.n, t.decay = x.weight_decay;
     };
+    const int large = state_bits == 32 ? UNIT : UNIT8, unit = units_of(params, count, large) >= ENOUGH ? large : SMALL_UNIT;
+    const bool wide = grad_dtype == FPDT_TW_F32;
     if (state_bits == 32) {
         AdamwArgs<Tensor32, TENSORS32> a;
         a.h = h;
-        return in_launches<decltype(a.list), TENSORS32>(params, count, UNIT, a.list, common, [&](unsigned units) {
-            if (grad_dtype == FPDT_TW_F32) adamw_kernel<float><<<units, 256, 0, st>>>(a);
-            else adamw_kernel<uint16_t><<<units, 256, 0, st>>>(a);
+        return in_launches<decltype(a.list), TENSORS32>(params, count, unit, a.list, common, [&](unsigned units) {
+            if (unit == UNIT && wide) adamw_kernel<float, UNIT><<<units, 256, 0, st>>>(a);
+            else if (unit == UNIT) adamw_kernel<uint16_t, UNIT><<<units, 256, 0, st>>>(a);
+            else if (wide) adamw_kernel<float, SMALL_UNIT><<<units, 256, 0, st>>>(a);
+            else adamw_kernel<uint16_t, SMALL_UNIT><<<units, 256, 0, st>>>(a);
         });
     }
     AdamwArgs<Tensor8, TENSORS8> a;
     a.h = h;
     return in_launches<decltype(a.list), TENSORS8>(
-        params, count, UNIT, a.list,
+        params, count, unit, a.list,
         [&](Tensor8& t, int k) {
             common(t, k);
             t.m_exp = params[k].m_exp, t.v_exp = params[k].v_exp, t.ordinal = (unsigned)k, t.pad = 0;
         },
         [&](unsigned units) {
-            if (grad_dtype == FPDT_TW_F32) adamw8_kernel<float><<<units, 256, 0, st>>>(a);
-            else adamw8_kernel<uint16_t><<<units, 256, 0, st>>>(a);
+            if (unit == UNIT8 && wide) adamw8_kernel<float, UNIT8><<<units, 256, 0, st>>>(a);
+            else if (unit == UNIT8) adamw8_kernel<uint16_t, UNIT8><<<units, 256, 0, st>>>(a);
+            else if (wide) adamw8_kernel<float, SMALL_UNIT><<<units, 256, 0, st>>>(a);
+            else adamw8_kernel<uint16_t, SMALL_UNIT><<<units, 256, 0, st>>>(a);
         });
 }
 
@@ -580,7 +604,7 @@ int fpdt_tw_adamw_unpack(const fpdt_tw_param* params, int count, void* stream)
     for (int k = 0; k < count; ++k) {
         const fpdt_tw_param& t = params[k];
         if (t.n < 0) return fail(TW_INVALID, "tensor %d has %lld elements", k, (long long)t.n);
-        if (t.n > (int64_t)UNIT * MOST_UNITS) return fail(TW_UNSUPPORTED, "tensor %d: %lld elements are beyond the launch limits", k, (long long)t.n);
+        if (t.n > MOST_ELEMENTS) return fail(TW_UNSUPPORTED, "tensor %d: %lld elements are beyond the launch limits", k, (long long)t.n);
         if (t.n && (!t.m || !t.v || !t.m_exp || !t.v_exp || !t.m_value || !t.v_value)) return fail(TW_INVALID, "tensor %d: NULL pointer", k);
         if (misaligned(t.m_value, 2) || misaligned(t.v_value, 2)) return fail(TW_INVALID, "tensor %d: a pointer is not aligned to its elements", k);
     }

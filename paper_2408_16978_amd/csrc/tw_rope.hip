@@ -198,11 +198,11 @@ template <class T, bool INTERLEAVED> __global__ __launch_bounds__(256) void rope
         const int wide = 256 * a.by_pairs >> 16;  // tokens at once: a thread keeps its pair
         const int tk = threadIdx.x * a.by_pairs >> 16, p = threadIdx.x - tk * half;
         if (tk < wide) {
-            const double f = a.freqs[p] * 0.15915494309189533577;
+            const double f = a.freqs[p];
             for (int k = tk; k < tokens; k += wide) {
                 const int64_t pos = a.positions ? a.positions[t0 + k] : a.position0 + t0 + k;
                 float sn, cs;
-                sincos_turns((double)pos * f, a.amplitude, sn, cs);
+                sincos_turns((double)pos * f * 0.15915494309189533577, a.amplitude, sn, cs);
                 table[k * half + p] = make_float2(cs, a.sign * sn);
             }
         }

@@ -77,7 +77,8 @@ def test_workspace_bytes_and_binding():
 # ------------------------------------------------------------------ GPU parity
 # (a lane of a wave, a quarter wave, several waves; cut-off accesses; one row; every shape of the kernels; the widest)
 SIZES = [(1, 1), (3, 5), (1, 4096), (67, 64), (1030, 128), (17, 129), (130, 513), (300, 512), (41, 1000), (2100, 257), (65, 2048), (33, 2560), (37, 4096), (9, 4099),
-         (11, 8192), (5, 12000), (3, 16384)]
+         (11, 8192), (5, 12000), (3, 16384),
+         (70, 200), (50, 384), (2101, 640), (1101, 2560), (40, 5120), (19, 6001), (1027, 1536)]
 
 
 def _make(rows, hidden, dtype, seed):

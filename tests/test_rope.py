@@ -127,7 +127,7 @@ def _check(name, got, ref, x, amplitude, dtype, rot, interleaved):
 
 SHAPES = [  # rows, Hq, Hkv, D, rot: accesses of 8, 4, 2 and 1 elements, one head and many, part of the head, one token
     (1, 8, 2, 128, 128), (33, 8, 2, 128, 128), (257, 4, 4, 80, 80), (100, 4, 1, 80, 32), (7, 5, 5, 64, 2), (65, 3, 1, 20, 10), (9, 2, 2, 6, 6),
-    (31, 1, 1, 7, 4), (1000, 32, 8, 64, 64), (3, 2, 1, 1024, 600), (2, 1, 1, 2050, 2050), (70000, 1, 1, 8, 8)]
+    (31, 1, 1, 7, 4), (1000, 32, 8, 64, 64), (33, 32, 8, 128, 34), (5000, 8, 2, 128, 30), (3, 200, 100, 16, 6), (50, 1, 1, 512, 6), (2100, 3, 3, 80, 20), (3, 2, 1, 1024, 600), (2, 1, 1, 2050, 2050), (70000, 1, 1, 8, 8)]
 
 
 @pytest.mark.gpu
@@ -215,6 +215,28 @@ def test_gpu_far_positions_keep_their_angle_and_negative_ones_turn_back():
     bad = ~torch.isfinite(z[:, 0])
     assert bad.nonzero().tolist() == [[0, 3], [0, 11], [1, 4], [1, 12]]
     assert torch.equal(z[~bad[:, None]], y[~bad[:, None]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rot", [64, 30])
+def test_gpu_tokens_far_apart(rot):
+    """Rows whose distance in a tile does not fit the short offsets: 2^26 elements, the last ones behind 2^31 bytes."""
+    rows, far = 20, (1 << 26) + 8
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GB")
+    big = torch.zeros((rows - 1) * far + 2 * 64, dtype=torch.bfloat16, device="cuda")
+    q = big.as_strided((rows, 2, 64), (far, 64, 1))
+    x = torch.randn(rows, 2, 64, device="cuda").to(torch.bfloat16)
+    q.copy_(x)
+    fd = TW.fpdt_tw_rope_freqs(rot, 10000.0).cuda()
+    near, out = torch.empty_like(x), torch.empty_like(x)
+    TW.fpdt_tw_rope_fwd(x, None, None, near, None, None, fd, position0=3)
+    TW.fpdt_tw_rope_fwd(q, None, None, out, None, None, fd, position0=3)
+    TW.fpdt_tw_rope_fwd(x, None, None, q, None, None, fd, position0=3)
+    torch.cuda.synchronize()
+    # (other accesses, but the same operations on each pair)
+    assert torch.equal(out, near) and torch.equal(q, near)
+    assert int(torch.count_nonzero(big)) == int(torch.count_nonzero(near))
 
 
 @pytest.mark.gpu
