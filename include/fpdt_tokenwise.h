@@ -174,7 +174,8 @@ int fpdt_tw_rope_freqs(int rot, double base, int scaling, double factor, double 
  *   dR [rows, hidden]: the gradient that reaches S by another way (the residual stream's), or NULL.  dX is the gradient
  *   of X and of R; it may be S, dY or dR itself.  dW and dB may be NULL to skip; without both no workspace is needed.
  *   workspace: device memory, 256-byte aligned, >= fpdt_tw_norm_bwd_workspace_bytes(...)
- * Arithmetic and sums in fp32; the order of the sums depends on the arguments alone.
+ * Arithmetic and sums in fp32 (a row whose sum of squares fp32 does not hold has rstd = 0); the order of the sums depends on
+ * the arguments alone.
  */
 enum { FPDT_TW_RMSNORM = 0, FPDT_TW_LAYERNORM = 1 };
 int fpdt_tw_norm_fwd(const void *X, const void *R, const void *W, const void *B, void *S, void *Y, float *stats,
@@ -217,9 +218,10 @@ int fpdt_tw_grad_norm(const fpdt_tw_param *params, int count, int grad_dtype, do
  * AdamW step over a list.  With g the gradient times *grad_scale (device, fp32; NULL: 1):
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *     p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),   w = bf16(p)
- * in fp32 (the factors in fp64, rounded to fp32).  Where *grad_scale is not finite nothing changes: a step whose gradients
- * overflowed is passed over.  lr_dev (fp32) and step_dev (int64, values below 1 count as 1) on the device replace lr and step
- * where they are given: a captured step reads them at every replay.
+ * in fp32 (the factors in fp64, rounded to fp32; in the root, a v that is no normal number counts as the smallest).  Where
+ * *grad_scale is not finite nothing changes: a step whose gradients overflowed is passed over.  lr_dev (fp32) and step_dev
+ * (int64, values below 1 count as 1) on the device replace lr and step where they are given: a captured step reads them at
+ * every replay.
  *   FPDT_TW_ADAMW_ZERO_GRAD  the gradients are set to zero in the same pass (in a step that is passed over, too)
  *   state_bits 8             in a block of 128, E is the exponent field of the block's largest |value| rounded up to three
  *                            fraction bits (at least 40; 255: a value is not finite, and the whole block becomes NaN); a code c > 0

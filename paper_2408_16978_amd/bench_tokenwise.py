@@ -1,6 +1,7 @@
 """Throughput and workspace of the token-wise chunked operations (include/fpdt_tokenwise.h) as a
-function of the chunk count, at Llama-8B layer shapes.  Prints one JSON line per (operation,
-chunk count).  `python -m paper_2408_16978_amd.bench_tokenwise [--rows 65536] [--chunks 1,4,16,64]`.
+function of the chunk count, at Llama-8B layer shapes, and of the operations around them that are
+not chunked (rotary positions with the QKV split, normalisation, gradient norm, AdamW) in bytes a
+second.  Prints one JSON line per (operation, chunk count).  `python -m paper_2408_16978_amd.bench_tokenwise [--rows 65536] [--chunks 1,4,16,64]`.
 """
 import argparse
 import json
@@ -28,6 +29,7 @@ def main():
     ap.add_argument("--n-model", type=int, default=4096)
     ap.add_argument("--n-ffn", type=int, default=14336)
     ap.add_argument("--n-qkv", type=int, default=6144, help="(Hq + 2 Hkv) * D")
+    ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--vocab", type=int, default=128256)
     ap.add_argument("--chunks", default="1,2,4,8,16,64")
     ap.add_argument("--iters", type=int, default=3)
@@ -74,6 +76,40 @@ def main():
                 del ws
                 rec.update(ms=round(ms, 3), tflops=round(flops / ms * 1e-9, 1))
             print(json.dumps(rec), flush=True)
+    del dW1, dW3, dW2, dWq, dWv, W1, W3, W2, Wq, Wv, X, dY, Y, dX, Yq, loss, lse
+    unchunked(rows, nm, nf, nq, a.head_dim, a.iters, bf)
+
+
+def unchunked(rows, nm, nf, nq, D, iters, bf):
+    """What a step does around the products: every array read or written once (bytes as in the headline of each line)."""
+    dev, Hq = "cuda", nm // D
+    Hkv = (nq // D - Hq) // 2
+    X, R, W, S, Y = bf(rows, nm), bf(rows, nm), bf(nm), bf(rows, nm), bf(rows, nm)
+    rstd, dW = torch.empty(rows, device=dev), torch.zeros(nm, device=dev)
+    ws = torch.empty(TW.fpdt_tw_norm_bwd_workspace_bytes(rows, nm), dtype=torch.uint8, device=dev)
+    tensor = 2 * rows * nm
+    ops = [("rms_norm_fwd", 4 * tensor, lambda: TW.fpdt_tw_norm_fwd(X, R, W, None, S, Y, rstd, 1e-5)),
+           ("rms_norm_bwd", 4 * tensor, lambda: TW.fpdt_tw_norm_bwd(S, W, rstd, X, R, Y, dW, None, workspace=ws))]
+    if Hkv > 0 and (Hq + 2 * Hkv) * D == nq:
+        qkv = bf(rows, nq)
+        parts = qkv.view(rows, Hq + 2 * Hkv, D).split([Hq, Hkv, Hkv], 1)
+        out = [torch.empty(rows, h, D, dtype=torch.bfloat16, device=dev) for h in (Hq, Hkv, Hkv)]
+        freqs = TW.fpdt_tw_rope_freqs(D, 500000.0).to(dev)
+        ops += [("rope_split_fwd", 4 * rows * nq, lambda: TW.fpdt_tw_rope_fwd(*parts, *out, freqs)),
+                ("rope_gather_bwd", 4 * rows * nq, lambda: TW.fpdt_tw_rope_bwd(*out, *parts, freqs))]
+    sizes = [nq * nm, nm * nm, nf * nm, nf * nm, nf * nm, nm, nm]  # a layer's weights
+    n = sum(sizes)
+    f = lambda dt=torch.float32, by=1: [torch.zeros(-(-k // by), dtype=dt, device=dev) for k in sizes]
+    lists = {32: TW.FpdtTwParams(g=f(), p=f(), m=f(), v=f(), w=f(torch.bfloat16)),
+             8: TW.FpdtTwParams(g=f(), p=f(), m=f(torch.uint8), v=f(torch.uint8), w=f(torch.bfloat16), m_exp=f(torch.uint8, TW.FPDT_TW_STATE_BLOCK),
+                                v_exp=f(torch.uint8, TW.FPDT_TW_STATE_BLOCK))}
+    norm, nws = torch.zeros(2, device=dev), torch.empty(TW.fpdt_tw_grad_norm_workspace_bytes(lists[32]), dtype=torch.uint8, device=dev)
+    ops += [("grad_norm_layer", 4 * n, lambda: TW.fpdt_tw_grad_norm(lists[32], 1.0, norm, nws)),
+            ("adamw_layer_32bit", 30 * n, lambda: TW.fpdt_tw_adamw_step(lists[32], 1e-4, 0.9, 0.95, 1e-8, 1)),
+            ("adamw_layer_8bit", 18 * n, lambda: TW.fpdt_tw_adamw_step(lists[8], 1e-4, 0.9, 0.95, 1e-8, 1))]
+    for name, nbytes, fn in ops:
+        ms = _time(fn, max(iters, 10))
+        print(json.dumps({"op": name, "rows": rows, "n_chunks": None, "ms": round(ms, 4), "tbytes_per_s": round(nbytes / ms * 1e-9, 2)}), flush=True)
 
 
 if __name__ == "__main__":

@@ -265,7 +265,7 @@ class _Param(ctypes.Structure):
 
 class FpdtTwParams:
     """A list of tensors for fpdt_tw_grad_norm and fpdt_tw_adamw_*: lists of the same length, made once and kept as long as
-    the tensors are where they are.  g: fp32 or bf16; p: fp32; w: bf16 or None; m, v: fp32, or uint8 with m_exp, v_exp [ceil(n / 128)]
+    the tensors are where they are.  g: fp32 or bf16; p: fp32; w: bf16 (each or all may be None); m, v: fp32, or uint8 with m_exp, v_exp [ceil(n / 128)]
     (all zero at first); m_value, v_value: bf16, for fpdt_tw_adamw_unpack; weight_decay: a number, or one for each tensor."""
 
     def __init__(self, g, p=None, m=None, v=None, w=None, m_exp=None, v_exp=None, m_value=None, v_value=None, weight_decay=0.0):
@@ -288,6 +288,8 @@ class FpdtTwParams:
             self.array[i].n, self.array[i].weight_decay = n, weight_decay[i]
             for k, (tensors, dtype) in given.items():
                 t = tensors[i]
+                if t is None and k == "w":
+                    continue
                 want = -(-n // FPDT_TW_STATE_BLOCK) if k in ("m_exp", "v_exp") else n
                 if t.dtype != dtype or t.device != self.device:
                     raise TypeError("fpdt_tw: %s[%d] must be %s on %s, got %s on %s" % (k, i, dtype, self.device, t.dtype, t.device))

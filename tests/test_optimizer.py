@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import kernel_resources
 from oracle import tokenwise as otw
 from paper_2408_16978_amd import tokenwise as TW
 
@@ -139,6 +140,14 @@ def test_lists_are_checked_where_they_are_made():
     with pytest.raises(ValueError, match="current device"):
         TW.fpdt_tw_adamw_unpack(TW.FpdtTwParams(**eight))
     assert ctypes.sizeof(TW._Param) == 88
+
+
+@pytest.mark.parametrize("source", ["tw_optim.hip", "tw_rope.hip", "tw_norm.hip"])
+def test_no_scratch_memory(source):
+    """What a thread has under way stays in registers; but for layer norms' backward over fp32 rows of more than 8192 columns,
+    whose rows do not fit those of 16 waves."""
+    found = {n: v[2] for n, v in kernel_resources.kernels(source).items() if v[2]}
+    assert all(n.startswith("norm_bwd_kernel<float, 0, 4, true") and b <= 64 for n, b in found.items()), found
 
 
 # ------------------------------------------------------------------ GPU parity
@@ -310,6 +319,25 @@ def test_gpu_a_step_whose_gradients_overflowed_is_passed_over(bits, scale):
     n = len(RAGGED)
     assert all((g == 0).all() for g in model.g) and all(torch.equal(a, b) for a, b in zip(was[n:], model.bits_of_all()[n:]))
     model.check_surroundings()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gpu_copies_of_some_tensors_only(bits):
+    """A tensor without a bf16 copy, and the same elements of it; lists that only the norm is taken of cannot be stepped."""
+    a, b = Model([500, 300], bits, seed=6), Model([500, 300], bits, seed=6)
+    more = {} if bits == 32 else dict(m_exp=b.me, v_exp=b.ve)
+    some = TW.FpdtTwParams(g=b.g, p=b.p, m=b.m, v=b.v, w=[None, b.w[1]], weight_decay=b.decay, **more)
+    was = b.w[0].clone()
+    TW.fpdt_tw_adamw_step(a.list, step=1, **HYPER)
+    TW.fpdt_tw_adamw_step(some, step=1, **HYPER)
+    torch.cuda.synchronize()
+    assert torch.equal(b.w[0], was) and torch.equal(a.w[1], b.w[1]) and all(torch.equal(x, y) for x, y in zip(a.p + a.m + a.v, b.p + b.m + b.v))
+    with pytest.raises(TW.FpdtTwError) as e:
+        TW.fpdt_tw_adamw_step(TW.FpdtTwParams(g=a.g), step=1, **HYPER)
+    assert e.value.status == 1
+    with pytest.raises(ValueError):
+        TW.fpdt_tw_adamw_step(a.list, step=1, grad_scale=torch.ones(2, device="cuda"), **HYPER)
 
 
 @pytest.mark.gpu
