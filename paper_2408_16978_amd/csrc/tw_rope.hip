@@ -5,7 +5,7 @@
 //
 // The angle is formed in 64 bits (at 2M tokens a 32-bit product is off by 0.1 rad), turned into turns and reduced to an
 // eighth of a turn there; sine and cosine of what is left are polynomials in 32 bits.  That is about 50 instructions a
-// pair, so a thread keeps its pairs' sines and cosines for all heads of its token: no table is read from memory.
+// pair, so a thread keeps its pairs' sines and cosines for all heads that it turns of its token: no table is read from memory.
 #include <cmath>
 
 #include "../../include/fpdt_tokenwise.h"
@@ -34,7 +34,7 @@ struct RopeArgs {
     const double* freqs;
     float amplitude, sign;  // sign: -1 in the backward
     int D, rot;
-    int slots, tokens;  // slots of a head, tokens of a workgroup
+    int slots, head_lanes, tokens;  // slots of a head, heads and tokens of a workgroup at a time
     int split;          // heads of a workgroup (of all three tensors together)
     int by_access, by_pairs;
     Unit unit[3];
@@ -64,7 +64,7 @@ template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_boun
     constexpr bool ONE = INTERLEAVED && V > 1;
     constexpr int PAIRS = ONE ? V / 2 : V, ACC = ONE ? 1 : 2, U = 4;
     const int turning = ONE ? a.rot / V : a.rot / 2 / V;
-    const int lane = threadIdx.x / a.slots;  // token of the workgroup
+    const int hl = threadIdx.x / a.slots % a.head_lanes, lane = threadIdx.x / (a.slots * a.head_lanes);  // head of its kind, token of the workgroup
     const int h0 = blockIdx.y * a.split;
     auto get = [](const T* p) { return LINES ? load_once<V>(p) : load<V>(p); };
     auto put = [](T* p, const Vec<T, V>& v) {
@@ -75,7 +75,7 @@ template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_boun
         const int64_t row = t0 + lane;
         if (lane >= a.tokens || row >= a.rows) continue;
         const int64_t pos = a.positions ? a.positions[row] : a.position0 + row;
-        for (int j = threadIdx.x - lane * a.slots; j < a.slots; j += 256) {
+        for (int j = threadIdx.x % a.slots; j < a.slots; j += 256) {
             const bool turns = j < turning;
             float sn[PAIRS], cs[PAIRS];
             int at[2];
@@ -100,16 +100,16 @@ template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_boun
                 const bool turn = turns && t < 2;
                 const T* in = static_cast<const T*>(a.in[t]) + row * a.in_row[t];
                 T* out = static_cast<T*>(a.out[t]) + row * a.out_row[t];
-                for (int h = from; h < to; h += U) {
+                for (int h = from + hl; h < to; h += U * a.head_lanes) {
                     Vec<T, V> x[U][ACC];
 #pragma unroll
                     for (int u = 0; u < U; ++u)
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (h + u < to && (c == 0 || turns)) x[u][c] = get(in + (int64_t)(h + u) * a.D + at[c]);
+                            if (h + u * a.head_lanes < to && (c == 0 || turns)) x[u][c] = get(in + (int64_t)(h + u * a.head_lanes) * a.D + at[c]);
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        if (h + u >= to) break;
+                        if (h + u * a.head_lanes >= to) break;
                         if (turn) {
                             float y[ACC * V];
 #pragma unroll
@@ -124,7 +124,7 @@ template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_boun
                         }
 #pragma unroll
                         for (int c = 0; c < ACC; ++c)
-                            if (c == 0 || turns) put(out + (int64_t)(h + u) * a.D + at[c], x[u][c]);
+                            if (c == 0 || turns) put(out + (int64_t)(h + u * a.head_lanes) * a.D + at[c], x[u][c]);
                     }
                 }
             }
@@ -258,19 +258,15 @@ template <class T, bool INTERLEAVED> __global__ __launch_bounds__(256) void rope
 
 constexpr int MOST_D = 8192, MOST_HEADS = 4096;
 
-// Two workgroups on a compute unit, by LDS that nobody uses, from 12 heads on: more of them push each other's lines out of the
-// caches between two accesses to a line (us with all | two, bf16: 256K tokens, 4 / 4 heads of 80, rot = 80 in halves 218 | 196, 32 interleaved 191 | 180,
-// 8 / 2 of 64 159 | 153, 64K, 32 / 8 of 128 interleaved 290 | 280; with fewer heads too little is in flight: 8 / 1 of 128, rot = 64 66 | 71, 1 / 1 of 128 73 | 88).
 template <class T, int V> void launch_v(const RopeArgs& a, bool interleaved, bool lines, dim3 grid, hipStream_t st)
 {
-    const size_t lds = a.heads[0] + a.heads[1] + a.heads[2] >= 12 ? 65536 : 0;
     if constexpr (V * sizeof(T) == 16) {
-        if (lines && interleaved) rope_kernel<T, V, true, true><<<grid, 256, lds, st>>>(a);
-        else if (lines) rope_kernel<T, V, false, true><<<grid, 256, lds, st>>>(a);
+        if (lines && interleaved) rope_kernel<T, V, true, true><<<grid, 256, 0, st>>>(a);
+        else if (lines) rope_kernel<T, V, false, true><<<grid, 256, 0, st>>>(a);
         if (lines) return;
     }
-    if (interleaved) rope_kernel<T, V, true, false><<<grid, 256, lds, st>>>(a);
-    else rope_kernel<T, V, false, false><<<grid, 256, lds, st>>>(a);
+    if (interleaved) rope_kernel<T, V, true, false><<<grid, 256, 0, st>>>(a);
+    else rope_kernel<T, V, false, false><<<grid, 256, 0, st>>>(a);
 }
 
 template <class T> void launch_any(RopeArgs& a, bool interleaved, hipStream_t st)
@@ -370,15 +366,24 @@ int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], c
         return TW_OK;
     }
     a.slots = (inter && v > 1 ? rot / v : rot / 2 / v) + (D - rot) / v;
-    a.tokens = a.slots >= 256 ? 1 : 256 / a.slots;
+    // Neighbouring lanes take neighbouring heads too, which keeps what a wave accesses together (64K tokens, us with 1 | 2 | 4 | 8 of them, bf16:
+    // 32 / 8 heads of 128 318 | 295 | 278 | 268, 8 / 2 71 | 70 | 68 | 89, 8 / 1 67 | 64 | 71 | 116; 256K tokens, 4 / 4 of 80 191 | 177 | 170 | 243), up to
+    // where a third of the lanes has no head; each takes its token's sines and cosines itself.
+    a.head_lanes = 1;
+    for (int n = 2; n <= 8 && n * a.slots <= 256; n *= 2) {
+        int passes = 0;
+        for (int h : a.heads) passes += (h + n - 1) / n;
+        if (3 * n * passes <= 4 * heads) a.head_lanes = n;
+    }
+    a.tokens = a.slots >= 256 ? 1 : 256 / (a.slots * a.head_lanes);
     // What the lanes of a token access: a head (interleaved), or a half and what is copied.
     bool lines = v == full && D * size % 128 == 0 && (inter || rot / 2 * size % 128 == 0);
     for (int t = 0; t < 3; ++t)
         lines = lines && !misaligned(a.in[t], 128) && !misaligned(a.out[t], 128) && a.in_row[t] * size % 128 == 0 && a.out_row[t] * size % 128 == 0;
     const int64_t tiles = (rows + a.tokens - 1) / a.tokens;
-    // All heads of a token in one thread, as long as that leaves every compute unit some workgroups.
+    // All heads of a token in one workgroup, as long as that leaves every compute unit some of them.
     int parts = tiles >= 1024 ? 1 : (int)((1024 + tiles - 1) / tiles);
-    if (parts > heads) parts = heads;
+    if (parts > (heads + a.head_lanes - 1) / a.head_lanes) parts = (heads + a.head_lanes - 1) / a.head_lanes;
     a.split = (heads + parts - 1) / parts;
     const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((heads + a.split - 1) / a.split));
     if (size == 4) {
