@@ -57,8 +57,8 @@ __device__ __forceinline__ void sincos_turns(double x, float amplitude, float& s
 
 // A slot of a head: V pairs in two accesses of V elements (halves; both layouts at V = 1), V / 2 pairs in one access
 // (interleaved, V > 1), and behind the rotated channels V elements that are copied.
-// LINES: what neighbouring lanes access are whole cache lines, which then go past the caches (65536 tokens, 8 / 2 heads of 128 in bf16 71 us
-// for 79, interleaved 32 / 8 289 for 311; where they are not, 4 / 4 heads of 80 226 for 185).
+// LINES: what neighbouring lanes access are whole cache lines, which then go past the caches (us for those through them, bf16: 64K tokens, 32 / 8
+// heads of 128 269 for 293, 256K tokens, 4 / 4 heads of 80 interleaved 161 for 170; where they are not lines, in halves, 245 for 195).
 template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
 {
     constexpr bool ONE = INTERLEAVED && V > 1;
@@ -376,8 +376,8 @@ int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], c
         if (3 * n * passes <= 4 * heads) a.head_lanes = n;
     }
     a.tokens = a.slots >= 256 ? 1 : 256 / (a.slots * a.head_lanes);
-    // What the lanes of a token access: a head (interleaved), or a half and what is copied.
-    bool lines = v == full && D * size % 128 == 0 && (inter || rot / 2 * size % 128 == 0);
+    // What the lanes of a token access: heads (interleaved), or a half and what is copied.
+    bool lines = v == full && (inter ? a.head_lanes : 1) * D * size % 128 == 0 && (inter || rot / 2 * size % 128 == 0);
     for (int t = 0; t < 3; ++t)
         lines = lines && !misaligned(a.in[t], 128) && !misaligned(a.out[t], 128) && a.in_row[t] * size % 128 == 0 && a.out_row[t] * size % 128 == 0;
     const int64_t tiles = (rows + a.tokens - 1) / a.tokens;
