@@ -169,8 +169,7 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const 
 }
 
 // Waves on a SIMD that the backward's registers are held to, and workgroups on the whole chip by that: one more than fit at
-// once would walk its rows when the others are done.  64K x 4096 in bf16 (8 waves a row): 768 workgroups 373 us, 512 and 1024 of
-// them 436 and 439.
+// once would walk its rows when the others are done.  64K x 4096 in bf16 (8 waves a row): 768 workgroups 373 us, 1024 of them 439, 1536 378.
 constexpr int bwd_waves(int accesses) { return accesses == 1 ? 6 : 4; }
 // Rows of partial sums, that is workgroups, at most: 16 MB of them, written and read again.
 constexpr int bwd_most(int hidden) { return hidden <= 2048 ? 2048 : 1024; }
@@ -312,7 +311,11 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, i
     d[c] += v;
 }
 
-// f(Shape, threads) for a row of n accesses of elements of T
+// f(Shape, threads) for a row of n accesses of elements of T.  Few accesses a lane keep registers free for rows under way; a wave's own row needs no
+// barrier, but the backward's partial sums are then added up in LDS.  Measured with 2^27 elements in bf16, us: forward, 128 accesses, two waves 166, one
+// with two 177; 1024 accesses, 8 waves with two 176, 16 with one 180.  Backward, 64 accesses, 64 lanes 180, 32 with two 192; 128 accesses,
+// 64 lanes with two 193, two waves 201; 256 accesses, 4 waves 189, two with two 196; 640 accesses, 10 waves 201, 5 with two 302 (of 5 waves, fewer
+// workgroups share a compute unit than registers would let).
 template <int L, int N> struct Shape {
     static constexpr int lanes = L, accesses = N;
 };
@@ -330,7 +333,7 @@ template <class T, class F> void bwd_shape(int n, F f)
 {
     if (n <= 16) f(Shape<16, 1>(), SMALL);
     else if (n <= 32) f(Shape<32, 1>(), SMALL);
-    else if (n <= 64) f(Shape<32, 2>(), SMALL);
+    else if (n <= 64) f(Shape<64, 1>(), SMALL);
     else if (n <= 128) f(Shape<64, 2>(), SMALL);
     else if (n <= 768) wide<1>(n, f);
     else if (n <= 2048) wide<2>(n, f);
