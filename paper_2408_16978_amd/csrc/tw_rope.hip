@@ -57,8 +57,8 @@ __device__ __forceinline__ void sincos_turns(double x, float amplitude, float& s
 
 // A slot of a head: V pairs in two accesses of V elements (halves; both layouts at V = 1), V / 2 pairs in one access
 // (interleaved, V > 1), and behind the rotated channels V elements that are copied.
-// LINES: what neighbouring lanes access are whole cache lines, which then go past the caches (us for those through them, bf16: 64K tokens, 32 / 8
-// heads of 128 269 for 293, 256K tokens, 4 / 4 heads of 80 interleaved 161 for 170; where they are not lines, in halves, 245 for 195).
+// LINES: what neighbouring lanes access are whole cache lines, which then go past the caches (us for those through them, bf16: 256K tokens, 1 / 1
+// heads of 128 in halves 69 for 77, 4 / 4 heads of 80 interleaved 161 for 170; where they are not lines, 4 / 4 of 80 in halves, 245 for 195).
 template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
 {
     constexpr bool ONE = INTERLEAVED && V > 1;
@@ -126,6 +126,80 @@ template <class T, int V, bool INTERLEAVED, bool LINES> __global__ __launch_boun
                         for (int c = 0; c < ACC; ++c)
                             if (c == 0 || turns) put(out + (int64_t)(h + u * a.head_lanes) * a.D + at[c], x[u][c]);
                     }
+                }
+            }
+        }
+    }
+}
+
+// Halves in accesses of 16 bytes: a lane has one access of a head, its pairs' other channels are in the lane `half / V` further.  What a
+// wave accesses lies together then, whatever D is.  The two lanes share their pairs' sines and cosines: each forms half of them.  64K tokens, 32 / 8 heads
+// of 128 257 us, 270 with a lane's halves in two accesses; 256K tokens, 8 / 2 of 64 131 for 147, 12 / 12 of 64 392 for 453, 4 / 4 of 80 177 for 194.
+// Past the caches in whole lines as above: 32 / 8 of 128 257 for 292.
+template <class T, bool LINES> __global__ __launch_bounds__(256) void rope_halves_kernel(RopeArgs a)
+{
+    constexpr int V = 16 / sizeof(T), H = V / 2, U = 4;
+    typedef Vec<T, V> Access;
+    const int lane = threadIdx.x & 63, sub = lane * a.by_access >> 16, acc = lane - sub * a.slots;  // head of the wave's, access of the head
+    const int per_wave = 64 / a.slots, group = threadIdx.x / 64 * per_wave + sub, token = group / a.head_lanes, hl = group % a.head_lanes;
+    const int far = a.rot / 2 / V, h0 = blockIdx.y * a.split;
+    const bool turns = acc < 2 * far, low = acc < far;
+    const int other = 4 * (lane + (low ? far : turns ? -far : 0));
+    auto swap = [&](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(other, __builtin_bit_cast(int, x))); };
+    auto get = [](const T* p) { return LINES ? load_once<V>(p) : load<V>(p); };
+    auto put = [](T* p, const Vec<T, V>& v) {
+        if (LINES) store_once(p, v);
+        else store(p, v);
+    };
+    for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.rows; t0 += (int64_t)gridDim.x * a.tokens) {
+        const int64_t row = t0 + token;
+        if (sub >= per_wave || token >= a.tokens || row >= a.rows) continue;  // (a head's lanes all the same)
+        const int64_t pos = a.positions ? a.positions[row] : a.position0 + row;
+        float sn[V], cs[V];
+        if (turns) {
+            const int p0 = (low ? acc : acc - far) * V + (low ? 0 : H);
+            float s[H], c[H];
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const double angle = (double)pos * a.freqs[p0 + i];
+                sincos_turns(angle * 0.15915494309189533577, a.amplitude, s[i], c[i]);
+                s[i] *= a.sign;
+            }
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const float so = swap(s[i]), co = swap(c[i]);
+                sn[i] = low ? s[i] : so, sn[H + i] = low ? so : s[i];
+                cs[i] = low ? c[i] : co, cs[H + i] = low ? co : c[i];
+            }
+        }
+        int before = 0;
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+            // heads [from, to) of this tensor belong to the workgroup
+            const int from = max(h0 - before, 0), to = min(h0 + a.split - before, a.heads[t]);
+            before += a.heads[t];
+            const T* in = static_cast<const T*>(a.in[t]) + row * a.in_row[t] + acc * V;
+            T* out = static_cast<T*>(a.out[t]) + row * a.out_row[t] + acc * V;
+            for (int h = from + hl; h < to; h += U * a.head_lanes) {
+                Vec<T, V> x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (h + u * a.head_lanes < to) x[u] = get(in + (int64_t)(h + u * a.head_lanes) * a.D);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (h + u * a.head_lanes >= to) break;
+                    if (t < 2 && turns) {
+                        uintx4 words = __builtin_bit_cast(uintx4, x[u]);
+                        const unsigned flip = low ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0;  // a cos - b sin, b cos + a sin
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) words[i] = (unsigned)__builtin_amdgcn_ds_bpermute(other, (int)words[i]) ^ flip;
+                        const Vec<T, V> o = __builtin_bit_cast(Access, words);
+                        float y[V];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) y[e] = fmaf(to_float(x[u].e[e]), cs[e], to_float(o.e[e]) * sn[e]);
+                        x[u] = rounded<V>(y, T());
+                    }
+                    put(out + (int64_t)(h + u * a.head_lanes) * a.D, x[u]);
                 }
             }
         }
@@ -366,18 +440,25 @@ int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], c
         return TW_OK;
     }
     a.slots = (inter && v > 1 ? rot / v : rot / 2 / v) + (D - rot) / v;
-    // Neighbouring lanes take neighbouring heads too, which keeps what a wave accesses together (64K tokens, us with 1 | 2 | 4 | 8 of them, bf16:
-    // 32 / 8 heads of 128 318 | 295 | 278 | 268, 8 / 2 71 | 70 | 68 | 89, 8 / 1 67 | 64 | 71 | 116; 256K tokens, 4 / 4 of 80 191 | 177 | 170 | 243), up to
-    // where a third of the lanes has no head; each takes its token's sines and cosines itself.
+    // Halves in accesses of 16 bytes go through rope_halves_kernel, but for those of whole cache lines with so few heads that the exchange of the
+    // sines shows (256K tokens, bf16, there | with two accesses a lane, us: 1 / 1 heads of 128 81 | 69, 2 / 2 131 | 131, back 136 | 131; 1 / 1 of 64 40 | 43,
+    // 1 / 1 of 80 54 | 58).
+    const bool halves = !inter && v == full && D / full <= 64 && (rot / 2 * size % 128 || heads > 6);
+    if (halves) a.slots = D / full, a.by_access = (65536 + a.slots - 1) / a.slots;
+    // Neighbouring lanes take neighbouring heads too, which keeps what a wave accesses together, up to where a third of the lanes has no head (64K
+    // tokens, 32 / 8 heads of 128 interleaved, us with 1 | 2 | 4 | 8 of them: 290 | 281 | 272 | 260; 256K tokens, 4 / 4 of 80 191 | 177 | 170 | 243); in halves, where
+    // sines and partners cost more, as long as a lane has six heads (64K, 32 / 8 of 128 294 | 284 | 276 | 257, 8 / 2 70 | 68 | 76; 256K, 8 / 2 of 64 140 | 131 | 148).
     a.head_lanes = 1;
     for (int n = 2; n <= 8 && n * a.slots <= 256; n *= 2) {
         int passes = 0;
         for (int h : a.heads) passes += (h + n - 1) / n;
-        if (3 * n * passes <= 4 * heads) a.head_lanes = n;
+        if (3 * n * passes <= 4 * heads && (!halves || passes >= 6)) a.head_lanes = n;
     }
-    a.tokens = a.slots >= 256 ? 1 : 256 / (a.slots * a.head_lanes);
+    const int groups = halves ? 4 * (64 / a.slots) : a.slots >= 256 ? 1 : 256 / a.slots;  // heads of a workgroup at a time
+    if (a.head_lanes > groups) a.head_lanes = groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
+    a.tokens = groups / a.head_lanes;
     // What the lanes of a token access: heads (interleaved), or a half and what is copied.
-    bool lines = v == full && (inter ? a.head_lanes : 1) * D * size % 128 == 0 && (inter || rot / 2 * size % 128 == 0);
+    bool lines = v == full && (inter || halves ? a.head_lanes : 1) * D * size % 128 == 0 && (inter || halves || rot / 2 * size % 128 == 0);
     for (int t = 0; t < 3; ++t)
         lines = lines && !misaligned(a.in[t], 128) && !misaligned(a.out[t], 128) && a.in_row[t] * size % 128 == 0 && a.out_row[t] * size % 128 == 0;
     const int64_t tiles = (rows + a.tokens - 1) / a.tokens;
@@ -386,7 +467,12 @@ int rope(const void* const in[3], const int64_t in_row[3], void* const out[3], c
     if (parts > (heads + a.head_lanes - 1) / a.head_lanes) parts = (heads + a.head_lanes - 1) / a.head_lanes;
     a.split = (heads + parts - 1) / parts;
     const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((heads + a.split - 1) / a.split));
-    if (size == 4) {
+    if (halves) {
+        if (size == 4 && lines) rope_halves_kernel<float, true><<<grid, 256, 0, st>>>(a);
+        else if (size == 4) rope_halves_kernel<float, false><<<grid, 256, 0, st>>>(a);
+        else if (lines) rope_halves_kernel<uint16_t, true><<<grid, 256, 0, st>>>(a);
+        else rope_halves_kernel<uint16_t, false><<<grid, 256, 0, st>>>(a);
+    } else if (size == 4) {
         if (v == 4) launch_v<float, 4>(a, inter, lines, grid, st);
         else if (v == 2) launch_v<float, 2>(a, inter, lines, grid, st);
         else launch_v<float, 1>(a, inter, lines, grid, st);

@@ -167,6 +167,41 @@ def test_gpu_split_and_gather_match_the_oracle(rows, Hq, Hkv, D, rot, dtype, int
     assert torch.equal(dv, Vo[:rows]) and (dX[:, (Hq + 2 * Hkv) * D:] == 3).all()
 
 
+HALVES = [  # a head's lanes: 3 (21 heads of a wave), 2, 6 (groups of heads across waves), 64 and 65 or 128, 12 of which 4 turn, 24 in fp32; heads that end inside a group
+    (67, 7, 3, 24, 16), (300, 17, 5, 16, 16), (129, 40, 24, 48, 32), (40, 33, 9, 512, 512), (5, 4, 2, 520, 512), (19, 9, 4, 256, 256), (2100, 12, 12, 96, 32),
+    (2, 64, 64, 64, 64), (1, 1, 1, 16, 16), (70, 2, 2, 128, 128), (70, 3, 2, 128, 128), (513, 1, 0, 80, 80), (66000, 2, 1, 24, 16)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,Hq,Hkv,D,rot", HALVES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gpu_halves_over_lanes(rows, Hq, Hkv, D, rot, dtype):
+    """Q and K there with given positions, in place as out of place, each pair within the parity tests' budget; K behind Q in a product's rows
+    (V is copied beside them); what lies between the heads' rows stays."""
+    print("[case] halves", rows, Hq, Hkv, D, rot, dtype, flush=True)
+    g = torch.Generator().manual_seed(rows + D)
+    H, freqs = Hq + 2 * Hkv, TW.fpdt_tw_rope_freqs(rot, 10000.0)
+    pos = torch.randint(-(1 << 20), 1 << 21, (rows,), generator=g)
+    X = torch.randn(rows, H * D + 3, generator=g).to(DT[dtype])
+    for sign, call in ((1, TW.fpdt_tw_rope_fwd), (-1, TW.fpdt_tw_rope_bwd)):
+        Xd, fd, pd = X.cuda(), freqs.cuda(), pos.cuda()
+        parts = lambda t: [t[:, a * D:b * D].unflatten(1, (b - a, D)) if b > a else None for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, H))]
+        q, k, v = parts(Xd)
+        outs = [None if t is None else torch.empty(t.shape, dtype=DT[dtype], device="cuda") for t in (q, k, v)]
+        call(q, k, v, *outs, fd, positions=pd, amplitude=0.75)
+        call(q, k, v, q, k, v, fd, positions=pd, amplitude=0.75)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, (q, k, v)) if a is not None)
+        assert torch.equal(Xd[:, H * D:].cpu(), X[:, H * D:])
+        for name, got, was in zip("QKV", outs, parts(X)):
+            if was is None or name == "V":
+                assert was is None or torch.equal(got.cpu(), was)
+                continue
+            x = was.double().numpy()
+            _check(name, got, otw.rope(x, pos.numpy(), freqs.numpy(), 0.75, inverse=sign < 0), x, 0.75, dtype, rot, False)
+            assert torch.equal(got[..., rot:].cpu(), was[..., rot:])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("off", [0, 1, 3])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
