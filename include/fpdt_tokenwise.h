@@ -134,7 +134,8 @@ enum { FPDT_TW_F32 = 0, FPDT_TW_BF16 = 1 };
  *   Q, K, V     [rows, Hq or Hkv, D] of `dtype`; the heads of a token are contiguous, tokens q_row, k_row, v_row elements
  *               apart (a slice of the QKV product: all (Hq + 2 Hkv) D).  K and V, or V alone, may be NULL (on both sides).
  *   Qo, Ko, Vo  the same, with distances of their own.  An output may be its own input (same address and distance: in place).
- *   freqs       rot / 2 radians per token, fp64, device;  even rot in [2, D], D <= 8192
+ *   freqs       rot / 2 radians per token, fp64, device;  even rot in [2, D], D <= 8192, at most 4096 heads and 2^31 - 1 rows, which are
+ *               at most 2^28 elements apart
  * Arithmetic in fp32, rounded once.
  */
 enum { FPDT_TW_ROPE_HALF = 0, FPDT_TW_ROPE_INTERLEAVED = 1 };
