@@ -266,7 +266,8 @@ class _Param(ctypes.Structure):
 class FpdtTwParams:
     """A list of tensors for fpdt_tw_grad_norm and fpdt_tw_adamw_*: lists of the same length, made once and kept as long as
     the tensors are where they are.  g: fp32 or bf16; p: fp32; w: bf16 (each or all may be None); m, v: fp32, or uint8 with m_exp, v_exp [ceil(n / 128)]
-    (all zero at first); m_value, v_value: bf16, for fpdt_tw_adamw_unpack; weight_decay: a number, or one for each tensor."""
+    (all zero at first); m_value, v_value: bf16, for fpdt_tw_adamw_unpack; weight_decay: a number, or one for each tensor.  The
+    tensors stay alive as long as this object does, whatever becomes of the lists that they came in."""
 
     def __init__(self, g, p=None, m=None, v=None, w=None, m_exp=None, v_exp=None, m_value=None, v_value=None, weight_decay=0.0):
         for k, tensors in (("g", g), ("p", p), ("m", m), ("v", v), ("w", w), ("m_exp", m_exp), ("v_exp", v_exp), ("m_value", m_value), ("v_value", v_value)):
@@ -302,7 +303,9 @@ class FpdtTwParams:
         for a, b in zip(taken, taken[1:]):
             if b[0] < a[1]:
                 raise ValueError("fpdt_tw: %s and %s overlap" % (a[2], b[2]))
-        self._keep = [tensors for tensors, _ in given.values()]
+        # the tensors, not the caller's lists of them, and the memory that they have now: neither a list that is changed later nor a
+        # `.data` that is replaced leaves an address of freed memory here
+        self._keep = [(t, t.untyped_storage()) for tensors, _ in given.values() for t in tensors if t is not None]
         self.address = ctypes.addressof(self.array)
 
     def _args(self):

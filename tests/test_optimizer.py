@@ -2,6 +2,7 @@
 GPU parity against the oracle."""
 import ctypes
 import math
+import weakref
 
 import numpy as np
 import pytest
@@ -140,6 +141,29 @@ def test_lists_are_checked_where_they_are_made():
     with pytest.raises(ValueError, match="current device"):
         TW.fpdt_tw_adamw_unpack(TW.FpdtTwParams(**eight))
     assert ctypes.sizeof(TW._Param) == 88
+
+
+def test_a_list_keeps_its_tensors_when_the_callers_lists_change():
+    """The library has their addresses: neither an emptied or refilled list nor a parameter that is given other memory may free them."""
+    z = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)
+    lists = dict(g=[z(300), z(40)], p=[z(300), z(40)], w=[None, z(40, torch.bfloat16)], m=[z(300, torch.uint8), z(40, torch.uint8)],
+                 v=[z(300, torch.uint8), z(40, torch.uint8)], m_exp=[z(3, torch.uint8), z(1, torch.uint8)], v_exp=[z(3, torch.uint8), z(1, torch.uint8)])
+    held = TW.FpdtTwParams(**lists)
+    refs = {(k, i): weakref.ref(t) for k, ts in lists.items() for i, t in enumerate(ts) if t is not None}
+    for k, ts in lists.items():
+        if k == "g":
+            ts[0] = z(300)
+        elif k != "p":
+            ts.clear()
+    p = lists["p"][1]
+    p.data = z(40)
+    assert p.data_ptr() != held.array[1].p
+    freed = [k for k, r in refs.items() if r() is None]
+    assert not freed, freed
+    # the memory as well, also where the tensor has another by now: what is taken from the allocator next lies elsewhere
+    taken = {t.data_ptr() for t in [z(40) for _ in range(64)]}
+    assert held.array[1].p not in taken
+    assert any(s.data_ptr() == held.array[1].p for _, s in held._keep)
 
 
 @pytest.mark.parametrize("source", ["tw_optim.hip", "tw_rope.hip", "tw_norm.hip"])
