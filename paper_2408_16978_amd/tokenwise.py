@@ -166,6 +166,17 @@ def _expect(name, t, shape, dtype, device):
     return t.data_ptr()
 
 
+def _room(workspace, device):
+    """Address and bytes of a workspace (None: none, which the library refuses where it needs one)."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        raise TypeError("fpdt_tw: the workspace must be on device %s, got %s" % (device, workspace.device))
+    if not workspace.is_contiguous():
+        raise ValueError("fpdt_tw: the workspace must be contiguous, got %s with strides %s" % (tuple(workspace.shape), workspace.stride()))
+    return workspace.data_ptr(), _nbytes(workspace)
+
+
 def _current(t):
     """The index of `t`'s device, which has to be the current one: calls go to its stream."""
     device = t.get_device()
@@ -254,7 +265,7 @@ def fpdt_tw_norm_bwd(S, W, stats, dY, dR, dX, dW, dB, kind=FPDT_TW_RMSNORM, work
     at = [None if t is None else _expect(name, t, shape, dtype, device) for name, t, shape in (
         ("S", S, S.shape), ("W", W, (hidden,)), ("dY", dY, S.shape), ("dR", dR, S.shape), ("dX", dX, S.shape))]
     sums = [None if t is None else _expect(name, t, (hidden,), torch.float32, device) for name, t in (("dW", dW), ("dB", dB))]
-    _check(load().fpdt_tw_norm_bwd(at[0], at[1], _stats(stats, rows, kind, device), *at[2:], *sums, rows, hidden, kind, code, _ptr(workspace), _nbytes(workspace),
+    _check(load().fpdt_tw_norm_bwd(at[0], at[1], _stats(stats, rows, kind, device), *at[2:], *sums, rows, hidden, kind, code, *_room(workspace, device),
                                    _raw_stream(stream, device)))
 
 
@@ -321,8 +332,8 @@ def fpdt_tw_grad_norm_workspace_bytes(params) -> int:
 def fpdt_tw_grad_norm(params, max_norm, out, workspace, stream=None):
     """out (fp32 [2]): norm of all gradients, and the factor that brings it down to max_norm."""
     args, device = params._args(), params.device.index
-    _check(load().fpdt_tw_grad_norm(*args, params.grad_dtype, max_norm, _expect("out", out, (2,), torch.float32, device), _ptr(workspace),
-                                    _nbytes(workspace), _raw_stream(stream, device)))
+    _check(load().fpdt_tw_grad_norm(*args, params.grad_dtype, max_norm, _expect("out", out, (2,), torch.float32, device), *_room(workspace, device),
+                                    _raw_stream(stream, device)))
 
 
 def fpdt_tw_adamw_step(params, lr, beta1, beta2, eps, step, lr_dev=None, step_dev=None, grad_scale=None, seed=0, flags=0, stream=None):
