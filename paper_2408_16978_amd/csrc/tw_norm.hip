@@ -171,12 +171,11 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const 
 // Waves on a SIMD that the backward's registers are held to, and workgroups on the whole chip by that: one more than fit at
 // once would walk its rows when the others are done.  64K x 4096 in bf16 (8 waves a row): 768 workgroups 373 us, 1024 of them 439, 1536 378.
 constexpr int bwd_waves(int accesses) { return accesses == 1 ? 6 : 4; }
-// Rows of partial sums, that is workgroups, at most: 16 MB of them, written and read again.
-constexpr int bwd_most(int hidden) { return hidden <= 2048 ? 2048 : 1024; }
+// Each leaves a row of partial sums for dw and one for db, which are read again: 16 MB a sum at most (512 rows of 8192 columns, 256 of 16384).
 constexpr int bwd_groups(int threads, int accesses, int hidden)
 {
-    const int n = 256 * (bwd_waves(accesses) * 4 / (threads / 64));
-    return n < bwd_most(hidden) ? n : bwd_most(hidden);
+    const int n = 256 * (bwd_waves(accesses) * 4 / (threads / 64)), most = hidden <= 2048 ? 2048 : 1024;
+    return n < most ? n : most;
 }
 
 // Groups of LANES threads walk the rows; a thread keeps its columns' shares of dw and db in registers, a workgroup's
@@ -339,6 +338,14 @@ template <class T, class F> void bwd_shape(int n, F f)
     else if (n <= 2048) wide<2>(n, f);
     else if constexpr (sizeof(T) == 4) wide<4>(n, f);
 }
+// The backward's workgroups on rows of `hidden` elements of T, where there are rows enough.
+template <class T> int bwd_most(int hidden)
+{
+    constexpr int V = 16 / sizeof(T);
+    int most = 0;
+    bwd_shape<T>((hidden + V - 1) / V, [&](auto shape, int threads) { most = bwd_groups(threads, decltype(shape)::accesses, hidden); });
+    return most;
+}
 // f(std::true_type or false_type) for each of two rules
 template <class F> void by_rule(bool a, bool b, F f)
 {
@@ -395,7 +402,7 @@ void launch_bwd(const void* S, const void* W, const float* stats, const void* dY
     auto t = [](const void* p) { return static_cast<const T*>(p); };
     bwd_shape<T>((hidden + V - 1) / V, [&](auto shape, int threads) {
         constexpr int L = decltype(shape)::lanes, N = decltype(shape)::accesses;
-        const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, bwd_groups(threads, N, hidden));
+        const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, bwd_most<T>(hidden));
         by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
             norm_bwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
                 <<<grid, threads, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
@@ -443,8 +450,9 @@ int fpdt_tw_norm_fwd(const void* X, const void* R, const void* W, const void* B,
 size_t fpdt_tw_norm_bwd_workspace_bytes(int64_t rows, int hidden, int kind)
 {
     if (rows <= 0 || hidden <= 0 || hidden > MOST_HIDDEN || rows > INT32_MAX || (kind != FPDT_TW_RMSNORM && kind != FPDT_TW_LAYERNORM)) return 0;
-    // one row of partial sums per workgroup, and never more workgroups than rows
-    return (size_t)groups_of(rows, 1, bwd_most(hidden)) * hidden * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
+    // one row of partial sums per workgroup, of the type that has more of them, and never more workgroups than rows
+    const int f = bwd_most<float>(hidden), b = bwd_most<uint16_t>(hidden);
+    return (size_t)groups_of(rows, 1, f > b ? f : b) * hidden * 4 * (kind == FPDT_TW_LAYERNORM ? 2 : 1);
 }
 
 int fpdt_tw_norm_bwd(const void* S, const void* W, const float* stats, const void* dY, const void* dR, void* dX, float* dW, float* dB, int64_t rows,

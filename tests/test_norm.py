@@ -74,6 +74,18 @@ def test_workspace_bytes_and_binding():
         TW.fpdt_tw_norm_fwd(x, None, x[0], None, None, x.clone(), None, 1e-5)
 
 
+def test_workspace_is_what_the_backward_writes():
+    """16 MiB for each of the sums at most, whatever the width (64 MiB were asked for at 16384 columns); as many workgroups as the widest launch of either
+    type has: as many as registers hold at once of 6 waves a SIMD with one access a lane (groups of 4 waves 6 a compute unit, of 8 three), or of 4 with more
+    (of 8 waves two, of 12 or 16 one)."""
+    W = TW.fpdt_tw_norm_bwd_workspace_bytes
+    for hidden in range(1, 16385):
+        assert 0 < W(1 << 20, hidden) <= 1 << 24 and W(1 << 20, hidden, TW.FPDT_TW_LAYERNORM) == 2 * W(1 << 20, hidden), hidden
+        assert W(5, hidden) == 5 * hidden * 4
+    groups = lambda hidden: W(1 << 20, hidden) // (4 * hidden)
+    assert [groups(h) for h in (64, 4096, 8192, 12288, 16384)] == [1536, 768, 512, 256, 256]
+
+
 # ------------------------------------------------------------------ GPU parity
 # (a lane of a wave, a quarter wave, several waves; cut-off accesses; one row; every shape of the kernels; the widest)
 SIZES = [(1, 1), (3, 5), (1, 4096), (67, 64), (1030, 128), (17, 129), (130, 513), (300, 512), (41, 1000), (2100, 257), (65, 2048), (33, 2560), (37, 4096), (9, 4099),
@@ -148,6 +160,30 @@ def test_gpu_forward_and_backward_match_the_oracle(rows, hidden, dtype, layer):
         TW.fpdt_tw_norm_bwd(S, W, stats, dY, dR, dX2, None, dB2, kind, ws)
         torch.cuda.synchronize()
         assert torch.equal(dB2, dB)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hidden", [64, 1001, 2048, 2056, 4096, 6144, 8192, 12288, 16384])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gpu_workspace_of_the_size_asked_for_and_no_more(hidden, dtype):
+    """More rows than there are workgroups (where a wave or less has a row, more than their rows): the bytes behind the workspace stay, and the sums of
+    small whole numbers, which fp32 adds exactly in any order, are all there."""
+    rows = 1600 if hidden > 1024 else 20000
+    g = torch.Generator(device="cuda").manual_seed(hidden)
+    S = torch.ones(rows, hidden, dtype=DT[dtype], device="cuda")
+    dY = torch.randint(-2, 3, (rows, hidden), device="cuda", generator=g).to(DT[dtype])
+    W, stats, dX = torch.ones(hidden, dtype=DT[dtype], device="cuda"), torch.zeros(2, rows, device="cuda"), torch.empty_like(S)
+    stats[1] = 1.0
+    need = TW.fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, TW.FPDT_TW_LAYERNORM)
+    room = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    dW, dB = torch.zeros(hidden, device="cuda"), torch.zeros(hidden, device="cuda")
+    TW.fpdt_tw_norm_bwd(S, W, stats, dY, None, dX, dW, dB, TW.FPDT_TW_LAYERNORM, room[:need])
+    torch.cuda.synchronize()
+    want = dY.double().sum(0)
+    assert (room[need:] == 77).all() and torch.equal(dW.double(), want) and torch.equal(dB.double(), want)
+    with pytest.raises(TW.FpdtTwError) as e:
+        TW.fpdt_tw_norm_bwd(S, W, stats, dY, None, dX, dW, dB, TW.FPDT_TW_LAYERNORM, room[:need - 1])
+    assert e.value.status == 3
 
 
 @pytest.mark.gpu
