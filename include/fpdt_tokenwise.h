@@ -219,7 +219,8 @@ int fpdt_tw_grad_norm(const fpdt_tw_param *params, int count, int grad_dtype, do
  * AdamW step over a list.  With g the gradient times *grad_scale (device, fp32; NULL: 1):
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *     p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),   w = bf16(p)
- * in fp32 (the factors in fp64, rounded to fp32; in the root, a v that is no normal number counts as the smallest).  Where
+ * in fp32 (the factors in fp64, rounded to fp32; root and quotient to half a step with 32-bit states, to a step of 2^-23 each with
+ * 8-bit states; in the root, a v that is no normal number counts as the smallest).  Where
  * *grad_scale is not finite nothing changes: a step whose gradients overflowed is passed over.  lr_dev (fp32) and step_dev
  * (int64, values below 1 count as 1) on the device replace lr and step where they are given: a captured step reads them at
  * every replay.

@@ -287,6 +287,40 @@ def test_gpu_hyperparameters_at_their_ends(bits, beta1, beta2, eps, lr):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("large", [False, True])
+def test_gpu_a_first_step_from_zero_is_the_rate_to_the_bit(large):
+    """Both betas 0, eps 0, a rate that is a power of two: v is g^2 rounded once, the root of which, rounded once, is |g|
+    again (short of overflow and underflow, as with any correctly rounded root), m times the rate is exact, and the quotient is the rate.  p is its
+    move then, and nothing else: root and quotient have to be right to half a step for this to hold for every g."""
+    model = Model([70000, 1, 4097] + ([4096 * 1024] if large else []), decay=0.5, fresh=True, seed=12)
+    for p, g in zip(model.p, model.g):
+        p.zero_()
+        g.mul_(torch.exp2(torch.randint(-20, 21, g.shape, device="cuda").float()))
+    TW.fpdt_tw_adamw_step(model.list, lr=2.0 ** -7, beta1=0.0, beta2=0.0, eps=0.0, step=1)
+    torch.cuda.synchronize()
+    for p, g in zip(model.p, model.g):
+        assert (g != 0).all() and torch.equal(p, -torch.sign(g) * 2.0 ** -7)
+
+
+@pytest.mark.gpu
+def test_gpu_moments_at_the_ends_of_the_range():
+    """g^2 beyond fp32 (v is infinite and the move none, as in fp32's own arithmetic), v that is no normal number, m so small that its move is none:
+    p stays a number, and as it was; a v that is not a number makes p none."""
+    model = Model([8], fresh=True, decay=0.0)
+    p, g, m, v = model.p[0], model.g[0], model.m[0], model.v[0]
+    g[:] = torch.tensor([1e30, -1e30, 0.0, 1e-30, 1e-22, 0.0, 0.0, 0.0], device="cuda")
+    v[:] = torch.tensor([0.0, 1e38, 1e-40, 0.0, 0.0, math.inf, math.nan, 0.0], device="cuda")
+    m[:] = torch.tensor([0.0, 0.0, 0.0, 0.0, 0.0, 3.0, 0.0, 0.0], device="cuda")
+    was = p.clone()
+    TW.fpdt_tw_adamw_step(model.list, step=1, **HYPER)
+    torch.cuda.synchronize()
+    assert torch.isnan(p).tolist() == [False] * 6 + [True, False]
+    assert torch.equal(p[[0, 1, 2, 5, 7]], was[[0, 1, 2, 5, 7]])
+    # (g^2 is lost, or all of it but its size; eps 1e-8 is what is left of the root: moves of 1e-24 and 1e-16 are none)
+    assert torch.equal(p[3:5], was[3:5]) and torch.isinf(v[[0, 1, 5]]).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("count", [1, 47, 49, 200])
 def test_gpu_many_tensors_norm_clip_step_and_zeroed_gradients(bits, count):
