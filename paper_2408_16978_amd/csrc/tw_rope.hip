@@ -40,13 +40,14 @@ struct RopeArgs {
     Unit unit[3];
 };
 
-// sin and cos of 2 pi x, times `amplitude`.  x is reduced to within 1/8 of a multiple of 1/4 in 64 bits; the remainders of
-// the Taylor series up to z^9 and z^10 at z = pi / 4 are below 2e-9 and 2e-10.
+// sin and cos of 2 pi x, times `amplitude`.  x is reduced to within 1/8 of a multiple of 1/4 and made an angle in 64 bits, which is rounded once; the
+// remainders of the Taylor series up to z^9 and z^10 at z = pi / 4 are below 2e-9 and 2e-10.  Right to 8e-8: half a step of the angle (3e-8 times at most 0.9), half
+// a step of the result, 2e-8 of the sums before it (1e-7 with the reduced x rounded, and then its product with 2 pi).
 __device__ __forceinline__ void sincos_turns(double x, float amplitude, float& s, float& c)
 {
     x -= rint(x);
     const double k = rint(4. * x);
-    const float z = 6.2831853071795864769f * (float)fma(-0.25, k, x), z2 = z * z;
+    const float z = (float)(6.2831853071795864769 * fma(-0.25, k, x)), z2 = z * z;
     const float ps = fmaf(z * z2, fmaf(z2, fmaf(z2, fmaf(z2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), z);
     const float pc = fmaf(z2, fmaf(z2, fmaf(z2, fmaf(z2, fmaf(z2, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
     const int q = (int)k & 3;  // quarter turns

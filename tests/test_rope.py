@@ -253,6 +253,28 @@ def test_gpu_far_positions_keep_their_angle_and_negative_ones_turn_back():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (64, True), (6, False)])
+def test_gpu_sines_and_cosines_to_their_last_steps(rot, interleaved):
+    """The pair (1, 0) becomes (cos t, sin t), in fp32 without another rounding.  The angle is reduced in 64 bits (positions up to 2^21: 2^-51 of 2^21 radians at
+    most, 1e-9) and rounded once to fp32: 2^-25 below pi / 4, times a slope of at most 0.88 where it is that much.  The result's own rounding is
+    2^-25.  Before it: for the cosine z^2 / 2 <= 0.31 with z^2 rounded to 2^-24 of itself (1.9e-8) and a factor near 1/2 to 2^-26 (times z^2: 0.9e-8), where the slope is
+    0.71 at most; for the sine z^3 / 6 <= 0.081 with three roundings of 2^-24 (1.5e-8).  The cosine: 2.1e-8 + 3.0e-8 + 1.9e-8 + 0.9e-8 + 0.1e-8 = 8.0e-8, the
+    sine 7.2e-8."""
+    rows, heads = 16384, 2
+    freqs = TW.fpdt_tw_rope_freqs(rot, 10000.0)
+    pos = torch.randint(0, 1 << 21, (rows,), generator=torch.Generator().manual_seed(rot))
+    x = torch.zeros(rows, heads, 64, device="cuda")
+    a, b = (np.s_[..., 0:rot:2], np.s_[..., 1:rot:2]) if interleaved else (np.s_[..., :rot // 2], np.s_[..., rot // 2:rot])
+    x[a] = 1.0
+    y = torch.empty_like(x)
+    TW.fpdt_tw_rope_fwd(x, None, None, y, None, None, freqs.cuda(), positions=pos.cuda(), layout=TW.FPDT_TW_ROPE_INTERLEAVED if interleaved else TW.FPDT_TW_ROPE_HALF)
+    torch.cuda.synchronize()
+    t = (pos.double()[:, None] * freqs)[:, None]
+    y = y.double().cpu()
+    assert (y[a] - t.cos()).abs().max() <= 8.0e-8 and (y[b] - t.sin()).abs().max() <= 8.0e-8
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rot", [64, 30])
 def test_gpu_tokens_far_apart(rot):
     """Rows whose distance in a tile does not fit the short offsets: 2^26 elements, the last ones behind 2^31 bytes."""
