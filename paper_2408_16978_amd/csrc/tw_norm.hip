@@ -85,16 +85,19 @@ template <class T, int V> __device__ __forceinline__ void forget(Vec<T, V>& v)
     __builtin_memcpy(&v, x, sizeof v);
 }
 
+// A sum over a row, divided by its length: rounded once, which a product with a 1 / hidden in fp32 is not (a constant row of 1000 then kept a deviation of 6e-5,
+// 2% of what eps = 1e-5 stands for).  inv is 1 / hidden, an argument of the kernel that costs no vector registers.
+__device__ __forceinline__ float mean_of(float sum, double inv) { return (float)(sum * inv); }
+
 // Rows of NA accesses of V elements a lane.
 template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
 __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats, int64_t rows,
-                                                                          int hidden, float eps)
+                                                                          int hidden, double inv, float eps)
 {
     constexpr int V = 16 / sizeof(T), ROWS = LANES ? SMALL / (LANES ? LANES : 1) : 1;
     __shared__ float red[2][1][16];
     RowSum<LANES, 1> sum{red};
     const int lanes = row_lanes<LANES>(), lane = row_lane<LANES>();
-    const float inv = 1.f / hidden;
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t row = r0 + row_of<LANES>(), at = row * hidden;
         const int width = row < rows ? hidden : 0;  // (lanes without a row take part in the sums)
@@ -130,7 +133,7 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const 
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[0] += to_float(x[i].e[e]);
             sum(v);
-            mean = v[0] * inv;
+            mean = mean_of(v[0], inv);
         }
         float v[1] = {0.f};
 #pragma unroll
@@ -144,7 +147,7 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const 
             }
         }
         sum(v);
-        const float rstd = 1.f / sqrtf(v[0] * inv + eps);
+        const float rstd = 1.f / sqrtf((float)(v[0] * inv + eps));
         if (stats && lane == 0 && width) {
             if (LAYER) stats[row] = mean;
             stats[(LAYER ? rows : 0) + row] = rstd;
@@ -183,14 +186,13 @@ constexpr int bwd_groups(int threads, int accesses, int hidden)
 // of sums in every call.
 template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
 __global__ __launch_bounds__((LANES ? SMALL : 1024), bwd_waves(NA)) void norm_bwd_kernel(const T* S, const T* W, const float* stats, const T* dY, const T* dR, T* dX,
-                                                                                         float* partial, int64_t rows, int hidden, bool want_w, bool want_b)
+                                                                                         float* partial, int64_t rows, int hidden, double inv, bool want_w, bool want_b)
 {
     constexpr int V = 16 / sizeof(T), ROWS = LANES ? SMALL / (LANES ? LANES : 1) : 1, N = LAYER ? 2 : 1;
     __shared__ float red[2][N][16];
     __shared__ float lds[LANES ? NA * V * SMALL : 1];
     RowSum<LANES, N> sum{red};
     const int lanes = row_lanes<LANES>(), lane = row_lane<LANES>();
-    const float inv = 1.f / hidden;
     Vec<T, V> w[NA];
     float dw[NA][V], db[NA][V];
 #pragma unroll
@@ -234,7 +236,7 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024), bwd_waves(NA)) void norm_bw
             }
         }
         sum(v);
-        const float along = v[0] * inv, level = LAYER ? v[N - 1] * inv : 0.f;
+        const float along = mean_of(v[0], inv), level = LAYER ? mean_of(v[N - 1], inv) : 0.f;
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int c = (i * lanes + lane) * V;
@@ -389,7 +391,7 @@ void launch_fwd(const void* X, const void* R, const void* W, const void* B, void
         const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, 1 << 21);
         by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
             norm_fwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
-                <<<grid, threads, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, eps);
+                <<<grid, threads, 0, st>>>(t(X), t(R), t(W), t(B), static_cast<T*>(S), static_cast<T*>(Y), stats, rows, hidden, 1. / hidden, eps);
         });
     });
 }
@@ -405,7 +407,7 @@ void launch_bwd(const void* S, const void* W, const float* stats, const void* dY
         const unsigned grid = groups_of(rows, L ? SMALL / (L ? L : 1) : 1, bwd_most<T>(hidden));
         by_rule(kind == FPDT_TW_LAYERNORM, hidden % V == 0, [&](auto layer, auto whole) {
             norm_bwd_kernel<T, L, N, decltype(layer)::value, decltype(whole)::value>
-                <<<grid, threads, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, dW, dB);
+                <<<grid, threads, 0, st>>>(t(S), t(W), stats, t(dY), t(dR), static_cast<T*>(dX), partial, rows, hidden, 1. / hidden, dW, dB);
         });
         if (dW || dB)
             norm_sums_kernel<<<dim3((hidden + 31) / 32, dW && dB ? 2 : 1), 1024, 0, st>>>(partial, (int)grid, hidden, dW ? dW : dB, dB);

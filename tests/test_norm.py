@@ -163,6 +163,33 @@ def test_gpu_forward_and_backward_match_the_oracle(rows, hidden, dtype, layer):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hidden", [3, 7, 100, 520, 1001, 2560, 5120, 12000, 16383])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gpu_means_of_equal_values_are_that_value(hidden, dtype):
+    """Rows of one whole number each, whose sums are whole numbers below 2^24 and so exact in fp32 in any order: a quotient rounded once is
+    the number itself, so no deviation is left (LAYERNORM: Y = B, whatever eps makes of a deviation), and a mean square of 1024 or 9 gives its root.
+    Backward, equal gradients on a row without deviation: nothing is left of them."""
+    value = torch.tensor([1000.0, -1000.0, 3.0, 0.0, 1.0], device="cuda")
+    X = value[:, None].expand(-1, hidden).to(DT[dtype]).contiguous()
+    W, B = torch.full((hidden,), 1.5, device="cuda").to(DT[dtype]), torch.randn(hidden, device="cuda").to(DT[dtype])
+    Y, stats = torch.empty_like(X), torch.empty(2, len(value), device="cuda")
+    TW.fpdt_tw_norm_fwd(X, None, W, B, None, Y, stats, 1e-5, TW.FPDT_TW_LAYERNORM)
+    torch.cuda.synchronize()
+    assert torch.equal(stats[0], value) and torch.equal(Y, B.expand_as(Y))
+    one = torch.ones_like(W)
+    dY, dX = X.clone(), torch.empty_like(X)
+    TW.fpdt_tw_norm_bwd(X, one, stats, dY, None, dX, None, None, TW.FPDT_TW_LAYERNORM)
+    torch.cuda.synchronize()
+    assert (dX == 0).all()
+    # RMSNORM without eps: the mean square is the number's square, and rstd one over the number
+    size = torch.tensor([32.0, -32.0, 3.0, 2.0 ** -60, 1.0], device="cuda")
+    X = size[:, None].expand(-1, hidden).to(DT[dtype]).contiguous()
+    TW.fpdt_tw_norm_fwd(X, None, one, None, None, Y, stats[0], 0.0)
+    torch.cuda.synchronize()
+    assert torch.equal(stats[0], 1.0 / size.abs()) and torch.equal(Y, torch.sign(size)[:, None].expand_as(Y).to(Y.dtype))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hidden", [64, 1001, 2048, 2056, 4096, 6144, 8192, 12288, 16384])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gpu_workspace_of_the_size_asked_for_and_no_more(hidden, dtype):
