@@ -80,17 +80,28 @@ def main():
     unchunked(rows, nm, nf, nq, a.head_dim, a.iters, bf)
 
 
+def split_of(nm, nq, D):
+    """Heads (Hq, Hkv) of a product of nq columns, or None where these are no whole heads of all three, or none that can be turned whole
+    (an odd D) or at all (D beyond 8192, more than 4096 of them)."""
+    Hq = nm // D if D > 0 else 0
+    Hkv = (nq // D - Hq) // 2 if Hq else 0
+    return (Hq, Hkv) if Hkv > 0 and (Hq + 2 * Hkv) * D == nq and D % 2 == 0 and D <= 8192 and max(Hq, Hkv) <= 4096 else None
+
+
 def unchunked(rows, nm, nf, nq, D, iters, bf):
-    """What a step does around the products: every array read or written once (bytes as in the headline of each line)."""
-    dev, Hq = "cuda", nm // D
-    Hkv = (nq // D - Hq) // 2
-    X, R, W, S, Y = bf(rows, nm), bf(rows, nm), bf(nm), bf(rows, nm), bf(rows, nm)
-    rstd, dW = torch.empty(rows, device=dev), torch.zeros(nm, device=dev)
-    ws = torch.empty(TW.fpdt_tw_norm_bwd_workspace_bytes(rows, nm), dtype=torch.uint8, device=dev)
-    tensor = 2 * rows * nm
-    ops = [("rms_norm_fwd", 4 * tensor, lambda: TW.fpdt_tw_norm_fwd(X, R, W, None, S, Y, rstd, 1e-5)),
-           ("rms_norm_bwd", 4 * tensor, lambda: TW.fpdt_tw_norm_bwd(S, W, rstd, X, R, Y, dW, None, workspace=ws))]
-    if Hkv > 0 and (Hq + 2 * Hkv) * D == nq:
+    """What a step does around the products: every array read or written once (bytes as in the headline of each line).  Widths that
+    an operation does not take are left out."""
+    dev, heads, ops = "cuda", split_of(nm, nq, D), []
+    room = TW.fpdt_tw_norm_bwd_workspace_bytes(rows, nm)  # (0: too wide)
+    if room:
+        X, R, W, S, Y = bf(rows, nm), bf(rows, nm), bf(nm), bf(rows, nm), bf(rows, nm)
+        rstd, dW = torch.empty(rows, device=dev), torch.zeros(nm, device=dev)
+        ws = torch.empty(room, dtype=torch.uint8, device=dev)
+        tensor = 2 * rows * nm
+        ops += [("rms_norm_fwd", 4 * tensor, lambda: TW.fpdt_tw_norm_fwd(X, R, W, None, S, Y, rstd, 1e-5)),
+                ("rms_norm_bwd", 4 * tensor, lambda: TW.fpdt_tw_norm_bwd(S, W, rstd, X, R, Y, dW, None, workspace=ws))]
+    if heads:
+        Hq, Hkv = heads
         qkv = bf(rows, nq)
         parts = qkv.view(rows, Hq + 2 * Hkv, D).split([Hq, Hkv, Hkv], 1)
         out = [torch.empty(rows, h, D, dtype=torch.bfloat16, device=dev) for h in (Hq, Hkv, Hkv)]
