@@ -55,6 +55,25 @@ def test_state_codes_of_the_oracle(signed):
         assert abs(np.corrcoef(a, b)[0, 1]) < 4 / 256 and abs(np.histogram(b, 16)[0] / 4096 - 1).max() < 5 / 64
 
 
+def _chances(n, seed, step, k):
+    """oracle.tokenwise.state_chances of many elements at once"""
+    def mix(x):
+        x = x ^ x >> np.uint64(15)
+        x = x * np.uint64(0xB7E15163) & low
+        x = x ^ x >> np.uint64(13)
+        x = x * np.uint64(0x93C467E3) & low
+        return x ^ x >> np.uint64(16)
+    low = np.uint64(2 ** 32 - 1)
+    key = otw._mix(otw._mix(otw._mix(seed ^ 0x243F6A88) ^ (step * 0x9E3779B1 % 2 ** 32)) ^ (k * 0x85A308D3 % 2 ** 32))
+    r = mix((np.arange(n, dtype=np.uint64) * np.uint64(0x9E3779B1) & low) ^ np.uint64(key)).astype(np.int64)
+    return (r % 65536) / 65536.0, (r // 65536) / 65536.0
+
+
+def test_chances_of_many_elements_are_those_of_the_oracle():
+    for args in ((3000, 11, 7, 2), (1, 2 ** 32 - 1, 1, 0)):
+        assert all(np.array_equal(a, b) for a, b in zip(_chances(*args), otw.state_chances(*args)))
+
+
 def test_state_bytes_of_huge_tiny_and_other_values():
     for signed in (True, False):
         x = np.zeros(384)
@@ -300,6 +319,92 @@ def test_gpu_a_first_step_from_zero_is_the_rate_to_the_bit(large):
     torch.cuda.synchronize()
     for p, g in zip(model.p, model.g):
         assert (g != 0).all() and torch.equal(p, -torch.sign(g) * 2.0 ** -7)
+
+
+def _check_long(model, before, step, scale, seed):
+    """_check_step for millions of elements, among which some m are the small difference of their terms.  p, and 32-bit states: as there.  8-bit states: m is
+    2^-22 of its terms' sizes off before it is rounded, which is 2^-22 terms / |m| of itself, and it is 8 to 16 steps: the decision may be the other one within
+    2^-18 terms / |m| of a step (v, whose terms have one sign: 2^-18).  Below the smallest code a step is that code, and m less than one.  A block whose largest
+    is as near to 1.875 of a power of two, where its exponent changes (bf16 gradients and codes have few bits, and meet it exactly), may have the other exponent:
+    the codes stand for the same values, but for the smallest."""
+    P, G, M, V = before
+    now = model.state()
+    for k, n in enumerate(model.sizes):
+        p, m, v = otw.adamw(P[k], G[k], M[k], V[k], weight_decay=model.decay[k], step=step, scale=scale, **HYPER)
+        m_terms = np.abs(HYPER["beta1"] * M[k]) + np.abs((1 - HYPER["beta1"]) * G[k] * scale)
+        root = np.sqrt(v / (1 - HYPER["beta2"] ** step)) + HYPER["eps"]
+        tol = 2.0 ** -22 * np.abs(P[k]) + HYPER["lr"] * 2.0 ** -20 * m_terms / (1 - HYPER["beta1"] ** step) / root
+        assert (np.abs(now[0][k] - p) <= tol).all(), k
+        assert torch.equal(model.w[k], model.p[k].to(torch.bfloat16))
+        if model.bits == 32:
+            assert (np.abs(now[2][k] - m) <= 2.0 ** -22 * m_terms).all() and (np.abs(now[3][k] - v) <= 2.0 ** -22 * v).all()
+            continue
+        chances = _chances(n, seed, step, k)
+        for got, x, terms, chance, exp, signed in ((now[2][k], m, m_terms, chances[0], model.me[k], True), (now[3][k], v, v, chances[1], model.ve[k], False)):
+            want, slack, e = otw.state_rounded(x, chance, signed)
+            exp, blocks = exp.cpu().numpy().astype(np.int64), -(-n // 128)
+            other = np.flatnonzero(exp != e)
+            whole = lambda a: np.concatenate([np.abs(a), np.zeros(blocks * 128 - n)]).reshape(blocks, 128).max(axis=1)[other] if n else a
+            border = 1.875 * 2.0 ** (np.minimum(exp, e)[other] - 127)
+            assert (np.abs(exp - e)[other] == 1).all() and (np.abs(whole(x) - border) <= 2.0 ** -22 * whole(terms)).all(), (k, other)
+            small = np.repeat(np.where(exp != e, 2.0 ** (np.maximum(exp, e) - 127 - (15 if signed else 31) + 1), 0.0), 128)[:n]
+            off = (got != want) & (np.abs(x) >= small)
+            near = slack[off] * np.abs(x[off]) <= 2.0 ** -18 * terms[off]
+            assert near.all() and (np.abs(got - want)[off] <= np.abs(want[off]) / 8 + 1e-30).all(), (k, off.sum())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grads", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("off", [0, 1])
+def test_gpu_lists_of_whole_large_units(bits, grads, off):
+    """Lists of 1024 units of 4096 elements (8-bit states: 2048) or more take other kernels than short ones: units that are whole, units that are cut off, tensors
+    of less than one, clipped, with cleared gradients, and passed over."""
+    print("[case] large units", bits, grads, off, flush=True)
+    unit = 4096 if bits == 32 else 2048
+    model = Model([unit * 1024 + 5, 0, unit + 1, 1, 3 * unit, unit - 1, 130], bits, grads, off=off, seed=bits + off)
+    scale = torch.tensor([math.nan], device="cuda")
+    was = model.bits_of_all()
+    step = lambda k, flags=0: TW.fpdt_tw_adamw_step(model.list, step=k, grad_scale=scale, seed=5, flags=flags, **HYPER)
+    step(4)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(was, model.bits_of_all()))
+    scale.fill_(0.5)
+    for k, flags in ((4, 0), (5, TW.FPDT_TW_ADAMW_ZERO_GRAD)):
+        before = model.state()
+        step(k, flags)
+        torch.cuda.synchronize()
+        _check_long(model, before, k, 0.5, 5)
+    assert all((g == 0).all() for g in model.g)
+    for g in model.g:
+        g.fill_(1.0)
+    scale.fill_(math.inf)
+    was = model.bits_of_all()
+    step(6, TW.FPDT_TW_ADAMW_ZERO_GRAD)
+    torch.cuda.synchronize()
+    n = len(model.sizes)
+    assert all((g == 0).all() for g in model.g) and all(torch.equal(a, b) for a, b in zip(was[n:], model.bits_of_all()[n:]))
+    if bits == 8:
+        TW.fpdt_tw_adamw_unpack(model.list)
+        torch.cuda.synchronize()
+        _, _, M, V = model.state()
+        assert all(np.array_equal(a.double().cpu().numpy(), b, equal_nan=True) for a, b in zip(model.mv + model.vv, M + V))
+    model.check_surroundings()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("most", [1e-3, 1e3, math.inf])
+@pytest.mark.parametrize("grads", [torch.float32, torch.bfloat16])
+def test_gpu_norm_and_factor_of_one_tensor(grads, most):
+    """One tensor, clipped and not: norm and factor each rounded once to fp32 (sums and roots in 64 bits; 1% of that for those)."""
+    g = [(torch.randn(37, device="cuda") * 0.01).to(grads)]
+    out, ws = torch.zeros(2, device="cuda"), torch.empty(8192, dtype=torch.uint8, device="cuda")
+    TW.fpdt_tw_grad_norm(TW.FpdtTwParams(g=g), most, out, ws)
+    torch.cuda.synchronize()
+    norm, factor = otw.grad_norm([g[0].double().cpu().numpy()], most)
+    assert (factor < 1) == (most < 1)
+    assert abs(out[0].item() - norm) <= 2.0 ** -24 * norm * 1.01
+    assert abs(out[1].item() - factor) <= 2.0 ** -24 * factor * 1.01
 
 
 @pytest.mark.gpu
