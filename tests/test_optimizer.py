@@ -322,9 +322,11 @@ def test_gpu_a_first_step_from_zero_is_the_rate_to_the_bit(large):
 
 
 def _check_long(model, before, step, scale, seed):
-    """_check_step for millions of elements, among which some m are the small difference of their terms.  p, and 32-bit states: as there.  8-bit states: m is
-    2^-22 of its terms' sizes off before it is rounded, which is 2^-22 terms / |m| of itself, and it is 8 to 16 steps: the decision may be the other one within
-    2^-18 terms / |m| of a step (v, whose terms have one sign: 2^-18).  Below the smallest code a step is that code, and m less than one.  A block whose largest
+    """_check_step for millions of elements, among which some m are the small difference of their terms, and for factors that are no power of two.  m: the
+    gradient times its factor, 1 - beta1 as a float, their product and the sum are four roundings of 2^-24, 2^-22 of the terms' sizes; v: the first
+    of them counts twice in the square, which is rounded itself, so 6 in all: 2^-21.  p: m's four, v's six halved, and root, quotient, products and factors: under 16,
+    2^-20.  8-bit states: m is 2^-22 terms / |m| of itself off before it is rounded, and it is 8 to 16 steps: the decision may be the other one within
+    2^-18 terms / |m| of a step (v, whose terms have one sign: 2^-17).  Below the smallest code a step is that code, and m less than one.  A block whose largest
     is as near to 1.875 of a power of two, where its exponent changes (bf16 gradients and codes have few bits, and meet it exactly), may have the other exponent:
     the codes stand for the same values, but for the smallest."""
     P, G, M, V = before
@@ -337,10 +339,10 @@ def _check_long(model, before, step, scale, seed):
         assert (np.abs(now[0][k] - p) <= tol).all(), k
         assert torch.equal(model.w[k], model.p[k].to(torch.bfloat16))
         if model.bits == 32:
-            assert (np.abs(now[2][k] - m) <= 2.0 ** -22 * m_terms).all() and (np.abs(now[3][k] - v) <= 2.0 ** -22 * v).all()
+            assert (np.abs(now[2][k] - m) <= 2.0 ** -22 * m_terms).all() and (np.abs(now[3][k] - v) <= 2.0 ** -21 * v).all()
             continue
         chances = _chances(n, seed, step, k)
-        for got, x, terms, chance, exp, signed in ((now[2][k], m, m_terms, chances[0], model.me[k], True), (now[3][k], v, v, chances[1], model.ve[k], False)):
+        for got, x, terms, chance, exp, signed in ((now[2][k], m, m_terms, chances[0], model.me[k], True), (now[3][k], v, 2 * v, chances[1], model.ve[k], False)):
             want, slack, e = otw.state_rounded(x, chance, signed)
             exp, blocks = exp.cpu().numpy().astype(np.int64), -(-n // 128)
             other = np.flatnonzero(exp != e)

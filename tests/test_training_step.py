@@ -2,9 +2,12 @@
 clipping of its gradients and two AdamW steps, against the same in 64 bits with autograd."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+import test_optimizer
+from oracle import tokenwise as otw
 from paper_2408_16978_amd import runner
 from paper_2408_16978_amd import tokenwise as TW
 
@@ -134,3 +137,35 @@ def test_gpu_layer_loss_gradients_clip_and_steps(bits):
             # from here on the reference has this layer's weights
             ref[name].data.copy_(layer.w[name].double().cpu())
             layer.p[name].copy_(layer.w[name].float())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gpu_each_step_is_that_of_its_own_gradients(bits):
+    """Three steps of the layer, each held to the oracle's step from the gradients, weights, moments and factor that it found: to the optimizer tests' tolerances,
+    which are roundings of fp32, where the comparison with another model's gradients (above) can only be as close as those are."""
+    gen = torch.Generator().manual_seed(5)
+    weights = {k: (1 + 0.1 * torch.randn(s, generator=gen)) if len(s) == 1 else torch.randn(s, generator=gen) * s[1] ** -0.5 for k, s in SHAPES.items()}
+    layer = Layer({k: t.to(torch.bfloat16) for k, t in weights.items()}, bits)
+    x = torch.randn(S, HIDDEN, generator=gen).to(torch.bfloat16).cuda()
+    target, freqs = torch.randint(0, VOCAB, (S,), generator=gen).int().cuda(), TW.fpdt_tw_rope_freqs(D, 10000.0).cuda()
+    # the same tensors as the optimizer tests hold them, with moments of their own
+    model = test_optimizer.Model.__new__(test_optimizer.Model)
+    model.bits, model.g, model.p, model.w = bits, *([t.view(-1) for t in d.values()] for d in (layer.g, layer.p, layer.w))
+    model.sizes, model.decay = [t.numel() for t in model.p], [0.1 if t.dim() == 2 else 0.0 for t in layer.p.values()]
+    zeros = lambda by, dt: [torch.zeros(-(-n // by), dtype=dt, device="cuda") for n in model.sizes]
+    state, more = (torch.float32, {}) if bits == 32 else (torch.uint8, dict(m_exp=zeros(128, torch.uint8), v_exp=zeros(128, torch.uint8)))
+    model.m, model.v, model.me, model.ve = zeros(1, state), zeros(1, state), more.get("m_exp"), more.get("v_exp")
+    layer.params = TW.FpdtTwParams(g=model.g, p=model.p, w=model.w, m=model.m, v=model.v, weight_decay=model.decay, **more)
+    assert HYPER == test_optimizer.HYPER
+    for k in (1, 2, 3):
+        layer.gradients(x, target, freqs, 0)
+        before = model.state()
+        assert all(np.abs(g).max() > 0 for g in before[1])
+        layer.step(k)
+        torch.cuda.synchronize()
+        # (each rounded once, as in the norm's own tests)
+        for got, want in zip(layer.out.tolist(), otw.grad_norm(before[1], MAX_NORM)):
+            assert abs(got - want) <= 2.0 ** -24 * want * 1.01, k
+        test_optimizer._check_long(model, before, k, layer.out[1].item(), 0)
+        assert all((g == 0).all() for g in model.g)
