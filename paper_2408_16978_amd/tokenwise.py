@@ -166,6 +166,10 @@ def _expect(name, t, shape, dtype, device):
     return t.data_ptr()
 
 
+# Sizes that the library takes as an int: ctypes would pass the lower 32 bits of larger ones, and with them another shape.
+_INT_BITS = 30
+
+
 def _room(workspace, device):
     """Address and bytes of a workspace (None: none, which the library refuses where it needs one)."""
     if workspace is None:
@@ -192,6 +196,8 @@ def _raw_stream(stream, device):
 
 def fpdt_tw_rope_freqs(rot, base, scaling=FPDT_TW_ROPE_PLAIN, factor=1.0, context=0.0, low=1.0, high=4.0):
     """[rot / 2] fp64 on the host: radians per token of each pair.  Copy it to the device once."""
+    if rot >> _INT_BITS:
+        raise FpdtTwError(1, "rot=%d must be even and in [2, 8192]" % rot)
     out = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64)
     _check(load().fpdt_tw_rope_freqs(rot, base, scaling, factor, context, low, high, out.data_ptr()))
     return out
@@ -219,6 +225,8 @@ def _rope(call, ins, outs, freqs, positions, position0, amplitude, layout, strea
             raise ValueError("fpdt_tw: %s must be %s with contiguous heads, got %s with strides %s" % (name, (rows, heads, D), tuple(t.shape), strides))
         args += (t.data_ptr(), strides[0] if rows > 1 else heads * D)
     half = freqs.numel()
+    if (Hq | Hkv | D | half) >> _INT_BITS:
+        raise FpdtTwError(2, "sizes beyond the launch limits")
     args += (None if positions is None else _expect("positions", positions, (rows,), torch.int64, device), position0,
              _expect("freqs", freqs, (half,), torch.float64, device), amplitude, rows, Hq, Hkv, D, 2 * half, layout, code, _raw_stream(stream, device))
     _check(call(*args))
@@ -240,6 +248,8 @@ def fpdt_tw_norm_fwd(X, R, W, B, S, Y, stats, eps, kind=FPDT_TW_RMSNORM, stream=
     rows (RMSNORM: rstd) or 2 rows (LAYERNORM: mean, rstd) values for the backward."""
     device, dtype, code = _current(X), X.dtype, _dtype_code(X)
     rows, hidden = X.shape
+    if hidden >> _INT_BITS:
+        raise FpdtTwError(2, "hidden=%d beyond the launch limits" % hidden)
     at = [None if t is None else _expect(name, t, shape, dtype, device) for name, t, shape in (
         ("X", X, X.shape), ("R", R, X.shape), ("W", W, (hidden,)), ("B", B, (hidden,)), ("S", S, X.shape), ("Y", Y, X.shape))]
     _check(load().fpdt_tw_norm_fwd(*at, _stats(stats, rows, kind, device), rows, hidden, kind, eps, code, _raw_stream(stream, device)))
@@ -255,13 +265,15 @@ def _stats(stats, rows, kind, device):
 
 
 def fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind=FPDT_TW_RMSNORM) -> int:
-    return int(load().fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind))
+    return 0 if hidden >> _INT_BITS else int(load().fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind))
 
 
 def fpdt_tw_norm_bwd(S, W, stats, dY, dR, dX, dW, dB, kind=FPDT_TW_RMSNORM, workspace=None, stream=None):
     """dX (written) = gradient through the norm plus dR (or None); dW, dB fp32 [hidden] (accumulated into, or None)."""
     device, dtype, code = _current(S), S.dtype, _dtype_code(S)
     rows, hidden = S.shape
+    if hidden >> _INT_BITS:
+        raise FpdtTwError(2, "hidden=%d beyond the launch limits" % hidden)
     at = [None if t is None else _expect(name, t, shape, dtype, device) for name, t, shape in (
         ("S", S, S.shape), ("W", W, (hidden,)), ("dY", dY, S.shape), ("dR", dR, S.shape), ("dX", dX, S.shape))]
     sums = [None if t is None else _expect(name, t, (hidden,), torch.float32, device) for name, t in (("dW", dW), ("dB", dB))]
