@@ -89,6 +89,17 @@ template <class T, int V> __device__ __forceinline__ void forget(Vec<T, V>& v)
 // 2% of what eps = 1e-5 stands for).  inv is 1 / hidden, an argument of the kernel that costs no vector registers.
 __device__ __forceinline__ float mean_of(float sum, double inv) { return (float)(sum * inv); }
 
+// 1 / sqrt(sum inv + eps), rounded once: the hardware's root to a step of 2^-23 and one step of Newton's in 64 bits (a root and a quotient in fp32 are
+// two roundings).  What the hardware takes for zero, and infinities, go through fp32's own.
+__device__ __forceinline__ float rstd_of(float sum, double inv, float eps)
+{
+    const double q = fma((double)sum, inv, (double)eps);
+    const float f = (float)q;
+    if (!(f >= 0x1p-126f && f < INFINITY)) return 1.f / sqrtf(f);
+    const double r = __builtin_amdgcn_rsqf(f);
+    return (float)fma(0.5 * r, fma(-r * r, q, 1.), r);
+}
+
 // Rows of NA accesses of V elements a lane.
 template <class T, int LANES, int NA, bool LAYER, bool WHOLE>
 __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const T* X, const T* R, const T* W, const T* B, T* S, T* Y, float* stats, int64_t rows,
@@ -147,7 +158,7 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024)) void norm_fwd_kernel(const 
             }
         }
         sum(v);
-        const float rstd = 1.f / sqrtf((float)(v[0] * inv + eps));
+        const float rstd = rstd_of(v[0], inv, eps);
         if (stats && lane == 0 && width) {
             if (LAYER) stats[row] = mean;
             stats[(LAYER ? rows : 0) + row] = rstd;

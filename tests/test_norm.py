@@ -190,6 +190,30 @@ def test_gpu_means_of_equal_values_are_that_value(hidden, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hidden", [1, 77, 520, 2560, 4096, 16384])
+@pytest.mark.parametrize("eps", [0.0, 1e-5, 0.25])
+def test_gpu_rstd_is_rounded_once(hidden, eps):
+    """Rows of whole numbers, whose squares' sums fp32 holds: rstd is the fp32 number next to 1 / sqrt(sum / hidden + eps).  And where there is none next to it: no
+    square at all, squares below the normal numbers, a sum that is infinite."""
+    g = torch.Generator(device="cuda").manual_seed(hidden)
+    X = torch.randint(-7, 8, (600, hidden), device="cuda", generator=g).float()
+    X[:, 0] = torch.randint(1, 100, (600,), device="cuda", generator=g).float()
+    W, Y, stats = torch.ones(hidden, device="cuda"), torch.empty_like(X), torch.empty(600, device="cuda")
+    TW.fpdt_tw_norm_fwd(X, None, W, None, None, Y, stats, eps)
+    torch.cuda.synchronize()
+    total = X.double().square().sum(1).cpu().numpy()
+    assert total.max() < 2 ** 24
+    want = (1.0 / np.sqrt(total / hidden + float(np.float32(eps)))).astype(np.float32)
+    assert np.array_equal(stats.cpu().numpy(), want)
+    X = X[:4].zero_()
+    X[1], X[2], X[3, 0] = 2.0 ** -68, 3e38, math.inf
+    TW.fpdt_tw_norm_fwd(X, None, W, None, None, Y[:4], stats[:4], 0.0)
+    torch.cuda.synchronize()
+    # (2^-136 is held to 13 bits, half a step of which is 2^-14 of it, half that of its root)
+    assert stats[0] == math.inf and abs(stats[1].item() * 2.0 ** -68 - 1) <= 2.0 ** -14 and stats[2] == 0 and stats[3] == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hidden", [64, 1001, 2048, 2056, 4096, 6144, 8192, 12288, 16384])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gpu_workspace_of_the_size_asked_for_and_no_more(hidden, dtype):
