@@ -175,8 +175,8 @@ int fpdt_tw_rope_freqs(int rot, double base, int scaling, double factor, double 
  *   dR [rows, hidden]: the gradient that reaches S by another way (the residual stream's), or NULL.  dX is the gradient
  *   of X and of R; it may be S, dY or dR itself.  dW and dB may be NULL to skip; without both no workspace is needed.
  *   workspace: device memory, 256-byte aligned, >= fpdt_tw_norm_bwd_workspace_bytes(...)
- * Arithmetic and sums in fp32 (a row whose sum of squares fp32 does not hold has rstd = 0); the order of the sums depends on
- * the arguments alone.
+ * Arithmetic and sums in fp32 (a row whose sum of squares fp32 does not hold has rstd = 0), but for the quotients and root of the statistics and
+ * the last sums of dW and dB, which are formed in fp64 and rounded once; the order of the sums depends on the arguments alone.
  */
 enum { FPDT_TW_RMSNORM = 0, FPDT_TW_LAYERNORM = 1 };
 int fpdt_tw_norm_fwd(const void *X, const void *R, const void *W, const void *B, void *S, void *Y, float *stats,

@@ -294,15 +294,15 @@ __global__ __launch_bounds__((LANES ? SMALL : 1024), bwd_waves(NA)) void norm_bw
     }
 }
 
-// dw[c] += sum over the n rows of partial sums (db: the same, behind them).  32 columns (a cache line) and 32 shares of the
-// rows a workgroup.
+// dw[c] += sum over the n rows of partial sums (db: the same, behind them), in 64 bits: rounded once, with what was there.  32 columns (a cache line)
+// and 32 shares of the rows a workgroup.
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, int n, int hidden, float* d0, float* d1)
 {
     constexpr int COLS = 32, SHARES = 1024 / COLS, U = 8;
-    __shared__ float part[SHARES][COLS];
+    __shared__ double part[SHARES][COLS];
     const int lane = threadIdx.x % COLS, w = threadIdx.x / COLS, c = blockIdx.x * COLS + lane;
     const float* p = partial + (int64_t)blockIdx.y * n * hidden + c;
-    float v = 0.f;
+    double v = 0;
     if (c < hidden) {
         int r = w;
         for (; r + (U - 1) * SHARES < n; r += U * SHARES) {
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, i
 #pragma unroll
     for (int i = 1; i < SHARES; ++i) v += part[i][lane];
     float* d = blockIdx.y == 0 ? d0 : d1;
-    d[c] += v;
+    d[c] = (float)(d[c] + v);
 }
 
 // f(Shape, threads) for a row of n accesses of elements of T.  Few accesses a lane keep registers free for rows under way; a wave's own row needs no

@@ -214,6 +214,27 @@ def test_gpu_rstd_is_rounded_once(hidden, eps):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 37, 500])
+@pytest.mark.parametrize("layer", [False, True])
+def test_gpu_sums_over_rows_of_a_workgroup_each_are_rounded_once(rows, layer):
+    """Rows of several waves, no more of them than workgroups: a partial sum is one row's dY (U is 1), so dW and dB are sums of fp32 numbers, added in 64 bits
+    and rounded once: half a step, and 2^-40 of the sum of sizes for the sums themselves."""
+    hidden, kind = 4096, TW.FPDT_TW_LAYERNORM if layer else TW.FPDT_TW_RMSNORM
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    S, W, stats = torch.ones(rows, hidden, device="cuda"), torch.ones(hidden, device="cuda"), torch.zeros(2 if layer else 1, rows, device="cuda")
+    stats[-1] = 1.0
+    dY, dX = torch.randn(rows, hidden, device="cuda", generator=g), torch.empty_like(S)
+    was = torch.randn(2, hidden, device="cuda", generator=g)
+    dW, dB = was[0].clone(), was[1].clone() if layer else None
+    ws = torch.empty(TW.fpdt_tw_norm_bwd_workspace_bytes(rows, hidden, kind), dtype=torch.uint8, device="cuda")
+    TW.fpdt_tw_norm_bwd(S, W, stats, dY, None, dX, dW, dB, kind, ws)
+    torch.cuda.synchronize()
+    for got, before in ((dW, was[0]), (dB, was[1])) if layer else ((dW, was[0]),):
+        want = before.double() + dY.double().sum(0)
+        assert ((got.double() - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -40 * dY.double().abs().sum(0)).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hidden", [64, 1001, 2048, 2056, 4096, 6144, 8192, 12288, 16384])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gpu_workspace_of_the_size_asked_for_and_no_more(hidden, dtype):
