@@ -233,7 +233,8 @@ int fpdt_tw_grad_norm(const fpdt_tw_param *params, int count, int grad_dtype, do
  *                            lower ones, of
  *                                mix(i * 0x9E3779B1 ^ key),  key = mix(mix(mix(seed ^ 0x243F6A88) ^ step * 0x9E3779B1) ^ k * 0x85A308D3)
  *                                mix(x): x ^= x >> 15; x *= 0xB7E15163; x ^= x >> 13; x *= 0x93C467E3; x ^ x >> 16
- *                            for element i of tensor k of the list, mod 2^32 (where i / 2^32 = h > 0 the key is mix(key + h)).
+ *                            for element i of tensor k of the list, mod 2^32 (where i / 2^32 = h > 0 the key is mix(key + h)).  Lists
+ *                            that are stepped with one seed round with the same bits: give each list of a model a seed of its own.
  * fpdt_tw_adamw_unpack writes what the 8-bit states stand for into m_value and v_value (bf16 holds it exactly).
  */
 enum { FPDT_TW_ADAMW_ZERO_GRAD = 1u << 0 };

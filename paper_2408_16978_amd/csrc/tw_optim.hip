@@ -279,6 +279,8 @@ template <class G, int U> __global__ __launch_bounds__(256) void adamw_kernel(Ad
 // least 40, so that no code stands for a denormal; 255: a value was not finite, the block's values are NaN).  A code c > 0
 // stands for the float of bits (E - D) 2^23 + c 2^20, c = 0 for zero: three fraction bits and the exponents from E - D to E,
 // D = 15 for m (and a sign), 31 for v.
+// Shifts and multiplications by turns, so that every bit of x reaches every bit of the result: the form, and the shifts 15, 13 and 16, in which
+// the published hash XXH32 ends, with other odd factors.
 __device__ __forceinline__ unsigned mix(unsigned x)
 {
     x ^= x >> 15;

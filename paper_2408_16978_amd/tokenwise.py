@@ -350,7 +350,7 @@ def fpdt_tw_grad_norm(params, max_norm, out, workspace, stream=None):
 
 def fpdt_tw_adamw_step(params, lr, beta1, beta2, eps, step, lr_dev=None, step_dev=None, grad_scale=None, seed=0, flags=0, stream=None):
     """One step.  lr_dev (fp32), step_dev (int64), grad_scale (fp32): one value each on the device, or None; lr and step are
-    ignored where lr_dev and step_dev are given."""
+    ignored where lr_dev and step_dev are given.  seed (8-bit states): a number of its own for each list of a model."""
     args, device, at = params._args(), params.device.index, []
     for name, t, dtype in (("lr_dev", lr_dev, torch.float32), ("step_dev", step_dev, torch.int64), ("grad_scale", grad_scale, torch.float32)):
         if t is not None and (t.dtype != dtype or t.get_device() != device or t.numel() != 1):
