@@ -16,6 +16,9 @@
  *                          count, forward and (recomputing) backward.
  *   fpdt_tw_rope_*         rotary positions and the split of the QKV product into Q, K, V.
  *   fpdt_tw_norm_*         residual add and RMS or layer normalisation.
+ *   fpdt_tw_affine_*       products with bias, activation and residual or gate behind them.
+ *   fpdt_tw_dropout_*      dropout and residual add, without a stored mask.
+ *   fpdt_tw_experts_*      feed-forward blocks of experts: tokens sorted by expert and back, and their products.
  *   fpdt_tw_grad_norm, fpdt_tw_adamw_*   norm of all gradients, the optimizer's step.
  *
  * The dense products run on this library's own bf16 MFMA kernels (csrc/tw_gemm.hip: operands
@@ -185,6 +188,94 @@ size_t fpdt_tw_norm_bwd_workspace_bytes(int64_t rows, int hidden, int kind);
 int fpdt_tw_norm_bwd(const void *S, const void *W, const float *stats, const void *dY, const void *dR, void *dX, float *dW,
                      float *dB, int64_t rows, int hidden, int kind, int dtype, void *workspace, size_t workspace_bytes,
                      void *stream);
+
+/*
+ * Product with bias, activation and residual or gate behind it, in one pass over the output.
+ *     z = X W^T + B                                    (fp32; B may be NULL)
+ *     FPDT_TW_JOIN_ADD    Y = act(z) + R               (R may be NULL)
+ *     FPDT_TW_JOIN_TIMES  Y = act(z) R                 (a gated block: R is the other product)
+ *     FPDT_TW_ACT_NONE z,   FPDT_TW_ACT_GELU z Phi(z) (exact, not the tanh form),   FPDT_TW_ACT_SILU z / (1 + exp(-z))
+ *   X [rows, n_in], W [n_out, n_in], B [n_out], R, Z, Y [rows, n_out]: bf16.  Z: z rounded, for the backward, or NULL.  Y may be R.
+ *   X and W must be 16-byte aligned where n_in is a multiple of 8 (they are read in place; copied otherwise).
+ *   workspace: device memory, 256-byte aligned, >= fpdt_tw_affine_workspace_bytes(...)
+ * The backward of what is behind the product (that of the product itself is fpdt_tw_linear_bwd with dZ for dY):
+ *     JOIN_ADD    dZ = dY act'(Z)                                    (R's gradient is dY)
+ *     JOIN_TIMES  dZ = dY act'(Z) R,   dR = dY act(Z)
+ *     dB[e] += sum over the rows of e of dZ                          (ACCUMULATED into the caller's fp32 [experts, n_out])
+ *   Z, R, dY in; dZ, dR out: bf16 [rows, n_out].  Z, R and dR may be NULL where the formulas do not read or want them; dZ too with ACT_NONE and
+ *   JOIN_ADD (where it is dY); dB may be NULL.  dZ and dR may each be Z, R or dY (not both the same).
+ *   offsets: NULL with experts = 1, or int32 [experts + 1] on the device as fpdt_tw_experts_sort writes them: the rows from offsets[e] on, up to
+ *   offsets[e + 1], are e's, and rows without an expert are neither read nor written.
+ *   workspace (where dB is given): >= fpdt_tw_affine_bwd_workspace_bytes(...)
+ * Arithmetic and sums in fp32, each output rounded once (dB: partial sums in fp32, added up in fp64); the order of the sums depends on the sizes and offsets alone.
+ */
+enum { FPDT_TW_ACT_NONE = 0, FPDT_TW_ACT_GELU = 1, FPDT_TW_ACT_SILU = 2 };
+enum { FPDT_TW_JOIN_ADD = 0, FPDT_TW_JOIN_TIMES = 1 };
+size_t fpdt_tw_affine_workspace_bytes(int64_t rows, int n_in, int n_out);
+int fpdt_tw_affine_fwd(const void *X, const void *W, const void *B, const void *R, void *Z, void *Y, int64_t rows, int n_in,
+                       int n_out, int act, int join, void *workspace, size_t workspace_bytes, void *stream);
+size_t fpdt_tw_affine_bwd_workspace_bytes(int64_t rows, int n_out, int experts);
+int fpdt_tw_affine_bwd(const void *Z, const void *R, const void *dY, void *dZ, void *dR, float *dB, int64_t rows, int n_out,
+                       int act, int join, const int32_t *offsets, int experts, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/*
+ * Dropout with the residual add behind it; nothing is stored for the backward, which makes the same choice again.
+ *     Y = keep X s + R,   dX = keep dY s              s = 65536 / (65536 - d),   d = p 65536 rounded to nearest even (p = 1: Y = R)
+ * Element i of the call is number first + i.  Number j is kept where its 16 random bits are >= d.  They are the half (j % 2: the upper) of
+ * word j / 2 % 4 of Philox4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) with the counter
+ * (b mod 2^32, b / 2^32, step mod 2^32, step / 2^32), b = j / 8, and the key (seed mod 2^32, seed / 2^32).  So a chunk of a sequence drops what the whole
+ * sequence would; give each layer a seed of its own.
+ *   X, R, Y, dY, dX [n] of `dtype`; R may be NULL.  Y may be X or R, dX may be dY.  What is dropped is 0 whatever X holds there.
+ *   0 <= p <= 1,  first >= 0,  first + n < 2^62.  step_dev (int64) on the device replaces step where it is given: a captured call reads it at every replay.
+ * Arithmetic in fp32, rounded once.
+ */
+int fpdt_tw_dropout_fwd(const void *X, const void *R, void *Y, int64_t n, int64_t first, double p, uint64_t seed, int64_t step,
+                        const int64_t *step_dev, int dtype, void *stream);
+int fpdt_tw_dropout_bwd(const void *dY, void *dX, int64_t n, int64_t first, double p, uint64_t seed, int64_t step,
+                        const int64_t *step_dev, int dtype, void *stream);
+
+/*
+ * Tokens to their experts and back.  Token t is sent to expert[t, j], j < top; any value outside [0, experts) sends it nowhere (padding, say), and
+ * the same expert twice sends it twice.
+ *   sort          offsets[e]: assignments to experts before e ([experts + 1], the last one: all that are sent);  place[t, j]: offsets[e] + how many
+ *                 assignments to the same e come before (t, j) in memory, or -1
+ *   gather_fwd    Xs[place[t, j]] = X[t];                          rows of Xs from offsets[experts] on are left as they were
+ *   gather_bwd    dX[t] = sum_j dXs[place[t, j]] + R[t]            (R may be NULL: what reaches X by another way; dX may be R)
+ *   combine_fwd   Y[t] = sum_j weight[t, j] Ys[place[t, j]] + R[t] (R may be NULL: the residual; Y may be R)
+ *   combine_bwd   dYs[place[t, j]] = weight[t, j] dY[t];           dweight[t, j] = dY[t] . Ys[place[t, j]], 0 where nothing is sent
+ *   expert, place int32 [rows, top], weight, dweight fp32 [rows, top], offsets int32: device memory
+ *   X, Y, R, dX, dY [rows, hidden], Xs, Ys, dXs, dYs [rows top, hidden] of `dtype`.  A place outside [0, rows top) counts as -1.  In combine_bwd dYs or
+ *   dweight may be NULL (Ys too, without dweight; weight, without dYs); dYs may be Ys.
+ *   experts <= 1024,  rows top < 2^31
+ *   workspace (sort): device memory, 256-byte aligned, >= fpdt_tw_experts_sort_workspace_bytes(rows top, experts)
+ * Arithmetic in fp32, rounded once; sums in the order of j.
+ */
+size_t fpdt_tw_experts_sort_workspace_bytes(int64_t assignments, int experts);
+int fpdt_tw_experts_sort(const int32_t *expert, int32_t *offsets, int32_t *place, int64_t rows, int top, int experts,
+                         void *workspace, size_t workspace_bytes, void *stream);
+int fpdt_tw_experts_gather_fwd(const void *X, const int32_t *place, void *Xs, int64_t rows, int top, int hidden, int dtype,
+                               void *stream);
+int fpdt_tw_experts_gather_bwd(const void *dXs, const int32_t *place, const void *R, void *dX, int64_t rows, int top, int hidden,
+                               int dtype, void *stream);
+int fpdt_tw_experts_combine_fwd(const void *Ys, const float *weight, const int32_t *place, const void *R, void *Y, int64_t rows,
+                                int top, int hidden, int dtype, void *stream);
+int fpdt_tw_experts_combine_bwd(const void *Ys, const float *weight, const int32_t *place, const void *dY, void *dYs,
+                                float *dweight, int64_t rows, int top, int hidden, int dtype, void *stream);
+
+/*
+ * The experts' products: fpdt_tw_affine_fwd for the rows of each expert with its own W [experts, n_out, n_in] and B [experts, n_out], and the
+ * products of its backward.  (What is behind the product: fpdt_tw_affine_bwd with the same offsets.)
+ *     dX = dY W[e]   (written, bf16; NULL to skip),   dW[e] += dY^T X over e's rows   (ACCUMULATED, fp32; NULL to skip)
+ *   X, dX [rows, n_in], R, Z, Y, dY [rows, n_out] in the order of the sort; rows from offsets[experts] on are neither read nor written.  offsets may say
+ *   anything: rows outside [0, rows) are not touched.  Y may be R.
+ *   n_in and n_out multiples of 8, X, W and dY 16-byte aligned, experts <= 1024.  No workspace.
+ */
+int fpdt_tw_experts_affine_fwd(const void *X, const void *W, const void *B, const void *R, void *Z, void *Y,
+                               const int32_t *offsets, int64_t rows, int experts, int n_in, int n_out, int act, int join,
+                               void *stream);
+int fpdt_tw_experts_linear_bwd(const void *X, const void *W, const void *dY, void *dX, float *dW, const int32_t *offsets,
+                               int64_t rows, int experts, int n_in, int n_out, void *stream);
 
 /*
  * One tensor of the optimizer.  A list of them is an array in HOST memory that is read before the call returns; all

@@ -174,3 +174,72 @@ def state_rounded(x, chance, signed):
     value = np.where(size >= least, np.floor(up) * grid, np.where(low, least, 0.0))
     slack = np.where(size >= least, np.abs(up - np.round(up)), np.abs(chance - size / least) if signed else 1.0)
     return np.where(np.repeat(exp, 128)[:n] == 255, np.nan, value * np.sign(x)), slack, exp.astype(np.int64)
+
+
+def activation(z, act):
+    """act(z) and its derivative: z itself, z Phi(z) or z / (1 + exp(-z))."""
+    z = np.asarray(z, dtype=np.float64)
+    if act == "gelu":
+        Phi = 0.5 * _erfc(-z / math.sqrt(2.0))
+        return z * Phi, Phi + z * np.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+    if act == "silu":
+        with np.errstate(over="ignore"):
+            s = 1.0 / (1.0 + np.exp(-z))
+        return z * s, s * (1.0 + z * (1.0 - s))
+    return z, np.ones_like(z)
+
+
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
+
+
+def affine(X, W, B=None, R=None, act="none", times=False):
+    """z = X W^T + B;  Y = act(z) + R or act(z) * R.  Returns dict Y, Z."""
+    Z = np.asarray(X, dtype=np.float64) @ np.asarray(W, dtype=np.float64).T + (0.0 if B is None else np.asarray(B, dtype=np.float64))
+    Y = activation(Z, act)[0]
+    if R is not None:
+        R = np.asarray(R, dtype=np.float64)
+        Y = Y * R if times else Y + R
+    return {"Y": Y, "Z": Z}
+
+
+def affine_behind_bwd(Z, R, dY, act="none", times=False):
+    """Gradient of what is behind the product: dict dZ, dR (times: of R, else dY itself), dB = the columns' sums of dZ."""
+    dY = np.asarray(dY, dtype=np.float64)
+    y, slope = activation(Z, act) if Z is not None else (None, np.ones_like(dY))
+    dZ = dY * slope * (np.asarray(R, dtype=np.float64) if times else 1.0)
+    return {"dZ": dZ, "dR": dY * y if times else dY, "dB": dZ.sum(axis=0)}
+
+
+def philox(counter, key, rounds=10):
+    """Philox4x32 (Salmon et al. 2011): four words of 32 bits for each counter [n, 4], under a key of two words."""
+    c = [np.asarray(counter)[:, i].astype(np.uint64) for i in range(4)]
+    k, low = [int(key[0]), int(key[1])], np.uint64(0xffffffff)
+    for _ in range(rounds):
+        a, b = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(b >> np.uint64(32)) ^ c[1] ^ np.uint64(k[0]), b & low, (a >> np.uint64(32)) ^ c[3] ^ np.uint64(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) % 2 ** 32, (k[1] + 0xBB67AE85) % 2 ** 32]
+    return np.stack(c, axis=1)
+
+
+def dropout_kept(n, first, p, seed, step):
+    """Which of the elements first .. first + n - 1 dropout keeps, and what it multiplies them with."""
+    j = np.arange(first, first + n, dtype=np.uint64)
+    b = np.unique(j // np.uint64(8))
+    s = step % 2 ** 64
+    counter = np.stack([b % np.uint64(2 ** 32), b // np.uint64(2 ** 32), np.full_like(b, s % 2 ** 32), np.full_like(b, s // 2 ** 32)], axis=1)
+    words = philox(counter, (seed % 2 ** 32, seed // 2 ** 32))
+    halves = np.stack([words & np.uint64(0xffff), words >> np.uint64(16)], axis=2).reshape(-1)
+    at = (j - b[0] * np.uint64(8)).astype(np.int64)
+    d = int(np.rint(p * 65536))
+    return halves[at] >= d, (65536 / (65536 - d) if d < 65536 else 0.0)
+
+
+def experts_sort(expert, experts):
+    """offsets [experts + 1] and place (the shape of expert): assignments in the order of experts, then as they come."""
+    flat = np.asarray(expert).reshape(-1)
+    place, offsets = np.full(flat.shape, -1, dtype=np.int64), [0]
+    for e in range(experts):
+        mine = np.nonzero(flat == e)[0]
+        place[mine] = offsets[-1] + np.arange(len(mine))
+        offsets.append(offsets[-1] + len(mine))
+    return np.array(offsets), place.reshape(np.shape(expert))

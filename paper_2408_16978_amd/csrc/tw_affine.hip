@@ -1,0 +1,661 @@
+// Products with bias, activation and residual or gate behind them, dense and for the rows of many experts, and what their backward
+// needs (include/fpdt_tokenwise.h: fpdt_tw_affine_*, fpdt_tw_experts_affine_fwd, fpdt_tw_experts_linear_bwd).
+//
+//     z = x W^T + b,   y = act(z) + r  or  act(z) r                          (W, b: of the row's expert)
+//     dz = dy act'(z) (r),   dr = dy act(z),   db += sum_rows dz
+//     dx = dy W,   dW += dy^T x                                              (for each expert's rows)
+//
+// The products run the tile loop of tw_gemm_tile.h.  An expert's rows are neighbours, from offsets[e] on; offsets are known to the
+// device alone, so a launch has as many workgroups as the rows could need, and each finds its expert and tile from them.
+#include <cmath>
+#include <type_traits>
+
+#include "../../include/fpdt_tokenwise.h"
+#include "tw_act.h"
+#include "tw_common.h"
+#include "tw_gemm.h"
+#include "tw_gemm_tile.h"
+
+namespace fpdt_tw {
+namespace {
+
+constexpr int MOST_EXPERTS = 1024;
+constexpr int MOST_WIDTH = 1 << 22;              // a lane's offset within a tile is kept in 32 bits
+constexpr int64_t MOST_ROWS = (int64_t)1 << 24;  // of one dense product
+
+// What is done behind a product, in fp32.  Pointers are to the first of the product's rows (B: columns).
+template <int ACT> struct Epilogue {
+    static constexpr bool any = true;
+    const uint16_t *B, *R;
+    uint16_t *Z, *Y;
+    bool times;  // R multiplies the activation, otherwise it is added to it
+    bool wide;   // rows come in aligned pieces of 16 bytes in all of them
+    __device__ __forceinline__ float act(float z) const { return act_of<ACT>(z); }
+    __device__ __forceinline__ void one(float z, int64_t at) const
+    {
+        if (Z) Z[at] = from_float<uint16_t>(z);
+        float y = act(z);
+        if (R) y = times ? y * to_float(R[at]) : y + to_float(R[at]);
+        Y[at] = from_float<uint16_t>(y);
+    }
+};
+
+template <int ACT, int WMT, int WNT>
+__global__ __launch_bounds__(NTHREAD, 1) void affine_kernel(Operand A, Operand B, int K, int M, int N, Units u, float* part, Epilogue<ACT> behind)
+{
+    Unit at;
+    if (!find_unit(u, at)) return;
+    const int unit_stages = at.is_part ? u.split_stages : K / STAGE_K;
+    auto part_of = [&](size_t elems) { return part + ((size_t)at.split * (unsigned)(u.tiles - u.whole) + (at.id - (unsigned)u.whole)) * elems; };
+    product_tile<false, false, false, false, WMT, WNT>(A, B, K, nullptr, N, M, N, at.tile_m, at.tile_n, (int)at.split * unit_stages, unit_stages, at.is_part, part_of, behind);
+}
+
+// The divided tiles of a product, as tw_split_sum_kernel adds them, and what is behind it.
+template <int ACT>
+__global__ __launch_bounds__(256) void affine_sum_kernel(const float* part, Units u, int first, int tm, int tn, int M, int N, Epilogue<ACT> behind)
+{
+    const unsigned i = (unsigned)first + blockIdx.y;
+    int tile_m, tile_n;
+    tile_of((unsigned)u.whole + i, (unsigned)u.tiles / (unsigned)u.tiles_n, (unsigned)u.tiles_n, tile_m, tile_n);
+    const int at = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;  // within the tile: tm * tn is a multiple of 1024
+    const int m = tile_m * tm + at / tn, n = tile_n * tn + at % tn;
+    if (m >= M || n >= N) return;
+    const size_t stride = (size_t)(u.tiles - u.whole) * tm * tn;
+    const float* p = part + (size_t)i * tm * tn + at;
+    floatx4 v = *reinterpret_cast<const floatx4*>(p);
+    for (int s = 1; s < u.splits; ++s) v += *reinterpret_cast<const floatx4*>(p + s * stride);
+    const int64_t c = (int64_t)m * N + n;
+    if (behind.wide) {  // (N is a multiple of 8)
+        if (behind.B) {
+            const auto b = load<4>(behind.B + n);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] += to_float(b.e[r]);
+        }
+        float y[4];
+        if (behind.Z) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = v[r];
+            store(behind.Z + c, rounded<4>(y, uint16_t()));
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = behind.act(v[r]);
+        if (behind.R) {
+            const auto j = load<4>(behind.R + c);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = behind.times ? y[r] * to_float(j.e[r]) : y[r] + to_float(j.e[r]);
+        }
+        store(behind.Y + c, rounded<4>(y, uint16_t()));
+    } else {
+        for (int r = 0; r < 4 && n + r < N; ++r) behind.one(v[r] + (behind.B ? to_float(behind.B[n + r]) : 0.f), c + r);
+    }
+}
+
+// ---- experts ------------------------------------------------------------------------------
+// Where expert e's rows begin and end, whatever the offsets say within the rows that there are.
+__device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int rows)
+{
+    const int o = offsets[e];
+    return o < 0 ? 0 : o < rows ? o : rows;
+}
+
+struct Groups {
+    const int32_t* offsets;
+    int experts, rows;
+};
+
+// Tile number `turn` of this XCD's share, of all experts' tiles of tm rows in their order: the expert, its rows, and the tile among its own.
+struct GroupTile {
+    int expert, first, rows, tile_m, tile_n;
+};
+__device__ __forceinline__ bool find_group(const Groups& g, int tm, unsigned tiles_n, GroupTile& at)
+{
+    // a lane counts the tile rows of `per` neighbouring experts
+    const int lane = threadIdx.x & 63, per = (g.experts + 63) / 64, e0 = lane * per;
+    auto rows_of = [&](int e) {
+        const int n = offset_of(g.offsets, e + 1, g.rows) - offset_of(g.offsets, e, g.rows);
+        return n > 0 ? n : 0;
+    };
+    unsigned mine = 0;
+#pragma unroll 4
+    for (int i = 0; i < per; ++i)
+        if (e0 + i < g.experts) mine += (unsigned)(rows_of(e0 + i) + tm - 1) / (unsigned)tm;
+    unsigned upto = mine;  // those of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned v = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += v;
+    }
+    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * tiles_n;
+    const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8, run = (total + 7) / 8, id = xcd * run + turn;
+    if (turn >= run || id >= total) return false;  // whole workgroup, before any barrier
+    const int owner = __builtin_ctzll(__ballot(upto * tiles_n > id));
+    unsigned base = (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), owner), tiles = 0;
+    int e = owner * per;
+    for (;; ++e) {
+        tiles = (unsigned)(rows_of(e) + tm - 1) / (unsigned)tm;
+        if ((base + tiles) * tiles_n > id || e + 1 >= g.experts) break;
+        base += tiles;
+    }
+    if (id - base * tiles_n >= tiles * tiles_n) return false;  // (offsets that do not ascend)
+    at.expert = (int)fpdt::uniform((unsigned)e);
+    at.first = (int)fpdt::uniform((unsigned)offset_of(g.offsets, e, g.rows));
+    at.rows = (int)fpdt::uniform((unsigned)rows_of(e));
+    tile_of(fpdt::uniform(id - base * tiles_n), fpdt::uniform(tiles), tiles_n, at.tile_m, at.tile_n);
+    return true;
+}
+
+template <int ACT, int WMT, int WNT>
+__global__ __launch_bounds__(NTHREAD, 1) void experts_affine_kernel(const uint16_t* X, const uint16_t* W, int n_in, int n_out, Groups g, Epilogue<ACT> behind)
+{
+    GroupTile t;
+    if (!find_group(g, 64 * WMT, ((unsigned)n_out + 64 * WNT - 1) / (64 * WNT), t)) return;
+    const int64_t out = (int64_t)t.first * n_out;
+    const Operand a = {X + (int64_t)t.first * n_in, n_in, t.rows}, b = {W + (int64_t)t.expert * n_out * n_in, n_in, n_out};
+    if (behind.B) behind.B += (int64_t)t.expert * n_out;
+    if (behind.R) behind.R += out;
+    if (behind.Z) behind.Z += out;
+    behind.Y += out;
+    product_tile<false, false, false, false, WMT, WNT>(a, b, n_in, nullptr, n_out, t.rows, n_out, t.tile_m, t.tile_n, 0, n_in / STAGE_K, false,
+                                                       [](size_t) { return (float*)nullptr; }, behind);
+}
+
+// dX of an expert's rows = dY W
+template <int WMT, int WNT>
+__global__ __launch_bounds__(NTHREAD, 1) void experts_dx_kernel(const uint16_t* dY, const uint16_t* W, uint16_t* dX, int n_in, int n_out, Groups g)
+{
+    GroupTile t;
+    if (!find_group(g, 64 * WMT, ((unsigned)n_in + 64 * WNT - 1) / (64 * WNT), t)) return;
+    const Operand a = {dY + (int64_t)t.first * n_out, n_out, t.rows}, b = {W + (int64_t)t.expert * n_out * n_in, n_in, n_in};
+    product_tile<false, true, false, false, WMT, WNT>(a, b, n_out, dX + (int64_t)t.first * n_in, n_in, t.rows, n_in, t.tile_m, t.tile_n, 0, n_out / STAGE_K, false,
+                                                      [](size_t) { return (float*)nullptr; }, Nothing());
+}
+
+// dW of an expert += dY^T X over its rows
+template <int WMT, int WNT>
+__global__ __launch_bounds__(NTHREAD, 1) void experts_dw_kernel(const uint16_t* X, const uint16_t* dY, float* dW, int n_in, int n_out, Groups g)
+{
+    const unsigned tiles_n = ((unsigned)n_in + 64 * WNT - 1) / (64 * WNT), tiles_m = ((unsigned)n_out + 64 * WMT - 1) / (64 * WMT);
+    const unsigned total = tiles_m * tiles_n * (unsigned)g.experts, run = (total + 7) / 8, xcd = blockIdx.x % 8, turn = blockIdx.x / 8, id = xcd * run + turn;
+    if (turn >= run || id >= total) return;
+    const unsigned e = id / (tiles_m * tiles_n);
+    const int first = (int)fpdt::uniform((unsigned)offset_of(g.offsets, (int)e, g.rows)), last = (int)fpdt::uniform((unsigned)offset_of(g.offsets, (int)e + 1, g.rows));
+    if (last <= first) return;
+    int tile_m, tile_n;
+    tile_of(id - e * (tiles_m * tiles_n), tiles_m, tiles_n, tile_m, tile_n);
+    const Operand a = {dY + (int64_t)first * n_out, n_out, n_out}, b = {X + (int64_t)first * n_in, n_in, n_in};
+    product_tile<true, true, true, true, WMT, WNT>(a, b, last - first, dW + (int64_t)e * n_out * n_in, n_in, n_out, n_in, tile_m, tile_n, 0, (last - first) / STAGE_K, false,
+                                                   [](size_t) { return (float*)nullptr; }, Nothing());
+}
+
+// ---- backward of what is behind a product -------------------------------------------------
+// dz = dy act'(z) (r), dr = dy act(z); the columns' sums of dz in fp32 before it is rounded.
+//
+// Bound by the memory: every tensor is read or written once, eight columns a lane.  A workgroup of `cols` x (256 / cols) threads walks the rows of its
+// slice and keeps its columns' sums in registers; where an expert's rows end in the slice they are left as a row of partial sums, number slice + expert
+// (no two pairs that meet have the same number), for affine_sums_kernel: no atomics, the same order of sums in every call.
+struct Backward {
+    const uint16_t *Z, *R, *dY;
+    uint16_t *dZ, *dR;
+    float* partial;  // or NULL: no sums
+    int64_t rows;
+    int n, experts, cols;
+    const int32_t* offsets;  // or NULL: all rows are one expert's
+    int64_t slice;           // rows of a slice
+};
+__device__ __forceinline__ int64_t start_of(const int32_t* offsets, int e, int64_t rows)
+{
+    if (!offsets) return e ? rows : 0;
+    return offset_of(offsets, e, (int)rows);
+}
+
+template <int ACT, bool TIMES, bool WHOLE> __global__ __launch_bounds__(256) void affine_bwd_kernel(Backward b)
+{
+    constexpr int V = 8, U = 2;
+    constexpr bool BEHIND = TIMES || ACT != FPDT_TW_ACT_NONE;
+    __shared__ float lds[256 * V];
+    const int tc = threadIdx.x % b.cols, tr = threadIdx.x / b.cols, lines = 256 / b.cols, c = ((int)blockIdx.x * b.cols + tc) * V, left = b.n - c;
+    const int64_t used = start_of(b.offsets, b.experts, b.rows);
+    int64_t row = (int64_t)blockIdx.y * b.slice;
+    const int64_t last = row + b.slice < used ? row + b.slice : used;
+    int e = 0;
+    for (int up = b.experts; up - e > 1;) {  // the last expert that begins at or before the slice
+        const int mid = (e + up) / 2;
+        if (start_of(b.offsets, mid, b.rows) <= row) e = mid;
+        else up = mid;
+    }
+    auto fetch = [&](const uint16_t* p, int64_t at) {
+        if (WHOLE || left >= V) return load_once<V>(p + at);
+        Vec<uint16_t, V> v;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v.e[i] = i < left ? p[at + i] : 0;
+        return v;
+    };
+    auto put = [&](uint16_t* p, int64_t at, const Vec<uint16_t, V>& v) {
+        if (WHOLE || left >= V) {
+            store_once(p + at, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < left) p[at + i] = v.e[i];
+        }
+    };
+    while (row < last) {
+        while (e + 1 < b.experts && start_of(b.offsets, e + 1, b.rows) <= row) ++e;  // experts without rows
+        int64_t end = start_of(b.offsets, e + 1, b.rows);
+        end = end > row && end < last ? end : last;
+        float sum[V] = {};
+        if (left > 0)
+            for (int64_t r0 = row + tr; r0 < end; r0 += U * lines) {
+                Vec<uint16_t, V> dy[U], z[U], r[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int64_t at = (r0 + k * lines) * b.n + c;
+                    if (r0 + k * lines >= end) break;
+                    dy[k] = fetch(b.dY, at);
+                    if (BEHIND && ACT != FPDT_TW_ACT_NONE) z[k] = fetch(b.Z, at);
+                    if (TIMES && ACT == FPDT_TW_ACT_NONE) z[k] = fetch(b.Z, at);
+                    if (TIMES) r[k] = fetch(b.R, at);
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int64_t at = (r0 + k * lines) * b.n + c;
+                    if (r0 + k * lines >= end) break;
+                    float dz[V], dr[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float g = to_float(dy[k].e[i]);
+                        if (BEHIND) {
+                            float y;
+                            const float slope = slope_of<ACT>(to_float(z[k].e[i]), y);
+                            dz[i] = g * slope;
+                            if (TIMES) dz[i] *= to_float(r[k].e[i]), dr[i] = g * y;
+                        } else {
+                            dz[i] = g;
+                        }
+                        sum[i] += dz[i];
+                    }
+                    if (b.dZ) put(b.dZ, at, rounded<V>(dz, uint16_t()));
+                    if (TIMES && b.dR) put(b.dR, at, rounded<V>(dr, uint16_t()));
+                }
+            }
+        if (b.partial) {
+            float* out = b.partial + ((int64_t)blockIdx.y + e) * b.n;
+#pragma unroll
+            for (int i = 0; i < V; ++i) lds[threadIdx.x * V + i] = sum[i];
+            __syncthreads();
+            for (int i = threadIdx.x; i < b.cols * V; i += 256) {
+                float v = 0.f;
+                for (int k = 0; k < lines; ++k) v += lds[k * b.cols * V + i];
+                const int col = (int)blockIdx.x * b.cols * V + i;
+                if (col < b.n) out[col] = v;
+            }
+            __syncthreads();
+        }
+        row = end;
+    }
+}
+
+// dB of expert blockIdx.y += its partial sums, in 64 bits: rounded once, with what was there.  32 columns and 32 shares of the sums a workgroup.
+__global__ __launch_bounds__(1024) void affine_sums_kernel(Backward b, float* dB)
+{
+    constexpr int COLS = 32, SHARES = 1024 / COLS, U = 8;
+    __shared__ double part[SHARES][COLS];
+    const int lane = threadIdx.x % COLS, w = threadIdx.x / COLS, c = blockIdx.x * COLS + lane, e = blockIdx.y;
+    const int64_t begin = start_of(b.offsets, e, b.rows), end = start_of(b.offsets, e + 1, b.rows);
+    if (end <= begin) return;
+    const int64_t first = begin / b.slice + e, n = (end - 1) / b.slice + e - first + 1;
+    const float* p = b.partial + first * b.n + c;
+    double v = 0;
+    if (c < b.n) {
+        int64_t r = w;
+        for (; r + (U - 1) * SHARES < n; r += U * SHARES) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = p[(r + u * SHARES) * b.n];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v += x[u];
+        }
+        for (; r < n; r += SHARES) v += p[r * b.n];
+    }
+    part[w][lane] = v;
+    __syncthreads();
+    if (w || c >= b.n) return;
+#pragma unroll
+    for (int i = 1; i < SHARES; ++i) v += part[i][lane];
+    float* d = dB + (int64_t)e * b.n + c;
+    *d = (float)(*d + v);
+}
+
+// ---- host side ----------------------------------------------------------------------------
+size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// f(Int<act>) for an activation that was checked
+template <class F> void by_act(int act, F f)
+{
+    if (act == FPDT_TW_ACT_GELU) f(Int<FPDT_TW_ACT_GELU>());
+    else if (act == FPDT_TW_ACT_SILU) f(Int<FPDT_TW_ACT_SILU>());
+    else f(Int<FPDT_TW_ACT_NONE>());
+}
+// f(Int<WMT>, Int<WNT>) for the tiles that plans have
+template <class F> void by_tile(int wmt, int wnt, F f)
+{
+    if (wnt == 2) f(Int<2>(), Int<2>());
+    else if (wmt == 4) f(Int<4>(), Int<4>());
+    else if (wmt == 3) f(Int<3>(), Int<4>());
+    else if (wmt == 2) f(Int<2>(), Int<4>());
+    else f(Int<1>(), Int<4>());
+}
+
+int check_sizes(int64_t rows, int n_in, int n_out)
+{
+    if (rows <= 0 || n_in <= 0 || n_out <= 0) return fail(TW_INVALID, "rows, n_in and n_out must be positive");
+    if (n_in > MOST_WIDTH || n_out > MOST_WIDTH || rows > INT32_MAX) return fail(TW_UNSUPPORTED, "sizes beyond the launch limits");
+    return TW_OK;
+}
+int check_kind(int act, int join)
+{
+    if (act < FPDT_TW_ACT_NONE || act > FPDT_TW_ACT_SILU) return fail(TW_INVALID, "unknown activation %d", act);
+    if (join != FPDT_TW_JOIN_ADD && join != FPDT_TW_JOIN_TIMES) return fail(TW_INVALID, "unknown join %d", join);
+    return TW_OK;
+}
+
+// A tensor of a call: what it is called, its bytes, whether it is written.
+struct Arg {
+    const char* name;
+    const void* p;
+    size_t bytes;
+    bool written;
+};
+// Two of them that overlap, one at least written, are refused, but for `same`: pairs that may be one tensor (not a part of it).
+int check_apart(const Arg* a, int n, const int (*same)[2], int nsame)
+{
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n; ++j) {
+            if (!a[i].p || !a[j].p || !(a[i].written || a[j].written) || !ranges_meet(a[i].p, a[i].bytes, a[j].p, a[j].bytes)) continue;
+            bool may = false;
+            for (int k = 0; k < nsame; ++k) may = may || (a[i].p == a[j].p && same[k][0] == i && same[k][1] == j);
+            if (!may) return fail(TW_INVALID, "%s and %s overlap", a[i].name, a[j].name);
+        }
+    return TW_OK;
+}
+
+// The dense product: its copies and partial sums in the workspace.  Copies are made where rows are no multiple of 16 bytes, of X for
+// PIECE rows at a time.
+constexpr int64_t PIECE = 32768;
+int pitch_of(int n) { return n <= 64 ? (n + 7) / 8 * 8 : (n + 63) / 64 * 64; }
+struct Layout {
+    int64_t piece;       // rows of a product
+    size_t w, x, parts;  // bytes
+};
+size_t parts_of(const Plan& p) { return p.u.splits > 1 ? (size_t)p.u.splits * (p.u.tiles - p.u.whole) * (64 * p.wmt) * (64 * p.wnt) * 4 : 0; }
+Plan plan_of(int64_t rows, int n_in, int n_out) { return plan_launch(rows, n_out, (n_in < SK ? SK : n_in) / SK); }
+Layout layout_of(int64_t rows, int n_in, int n_out)
+{
+    Layout l = {};
+    const bool copy = n_in % 8 != 0;
+    l.piece = copy ? PIECE : MOST_ROWS;
+    if (copy) l.w = al256((size_t)n_out * pitch_of(n_in) * 2), l.x = al256((size_t)(rows < PIECE ? rows : PIECE) * pitch_of(n_in) * 2);
+    for (int64_t n : {rows < l.piece ? rows : l.piece, rows % l.piece})
+        if (n > 0) {
+            const size_t b = al256(parts_of(plan_of(n, n_in, n_out)));
+            if (b > l.parts) l.parts = b;
+        }
+    return l;
+}
+
+bool all_wide(int n, std::initializer_list<const void*> every)
+{
+    for (const void* p : every)
+        if (misaligned(p, 16)) return false;
+    return n % 8 == 0;
+}
+
+// Tiles for experts' products of about rows / experts rows each: the cheapest by launch_cost's measure, without divided tiles.
+struct GroupPlan {
+    int wmt, wnt;
+    int64_t tiles;  // at most, whatever the offsets
+};
+GroupPlan plan_groups(int64_t rows, int experts, int N, int K)
+{
+    static const int shapes[][2] = {{4, 4}, {3, 4}, {2, 4}, {1, 4}, {2, 2}};
+    GroupPlan best = {4, 4, 0};
+    double best_cost = 0;
+    const int64_t busy = rows < experts ? rows : experts;
+    for (const auto& sh : shapes) {
+        const int64_t tiles_n = (N + 64 * sh[1] - 1) / (64 * sh[1]), tm = 64 * sh[0], each = ((rows + busy - 1) / busy + tm - 1) / tm, tiles = each * busy * tiles_n;
+        const int slots = sh[0] * sh[1] <= 4 ? 512 : 256;
+        const double c = launch_cost(sh[0], sh[1], (double)(tiles / slots * slots), (double)(tiles % slots), 1, (K < SK ? SK : K) / SK);
+        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], (rows / tm + busy) * tiles_n}, best_cost = c;
+    }
+    return best;
+}
+GroupPlan plan_weights(int64_t rows, int experts, int n_in, int n_out)
+{
+    static const int shapes[][2] = {{4, 4}, {3, 4}, {2, 4}, {1, 4}, {2, 2}};
+    GroupPlan best = {4, 4, 0};
+    double best_cost = 0;
+    const int64_t busy = rows < experts ? rows : experts, K = (rows + busy - 1) / busy;
+    for (const auto& sh : shapes) {
+        const int64_t each = (int64_t)((n_in + 64 * sh[1] - 1) / (64 * sh[1])) * ((n_out + 64 * sh[0] - 1) / (64 * sh[0])), tiles = each * busy;
+        const int slots = sh[0] * sh[1] <= 4 ? 512 : 256;
+        const double c = launch_cost(sh[0], sh[1], (double)(tiles / slots * slots), (double)(tiles % slots), 1, (int)((K < SK ? SK : K) / SK));
+        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], each * experts}, best_cost = c;
+    }
+    return best;
+}
+unsigned grid_of(int64_t tiles) { return 8u * (unsigned)((tiles + 7) / 8); }
+
+int check_experts(int64_t rows, int experts, int n_in, int n_out)
+{
+    int rc = check_sizes(rows, n_in, n_out);
+    if (rc != TW_OK) return rc;
+    if (experts <= 0) return fail(TW_INVALID, "experts must be positive");
+    if (experts > MOST_EXPERTS) return fail(TW_UNSUPPORTED, "experts=%d beyond %d", experts, MOST_EXPERTS);
+    if (n_in % 8 || n_out % 8) return fail(TW_UNSUPPORTED, "n_in=%d and n_out=%d of experts must be multiples of 8", n_in, n_out);
+    return TW_OK;
+}
+
+int lanes_of(int n)
+{
+    int cols = 8;
+    while (cols < 256 && cols * 8 < n) cols *= 2;
+    return cols;
+}
+// Rows of a slice: 2048 workgroups where there are rows enough, so that partial sums stay a small part of the tensors, and two rows a thread at least.
+int64_t slice_of(int64_t rows, int n)
+{
+    const int cols = lanes_of(n), wide = (n + cols * 8 - 1) / (cols * 8);
+    const int64_t most = wide < 2048 ? 2048 / wide : 1, slice = (rows + most - 1) / most, least = 2 * (256 / cols);
+    return slice > least ? slice : least;
+}
+
+}  // namespace
+}  // namespace fpdt_tw
+
+using namespace fpdt_tw;
+
+extern "C" {
+
+size_t fpdt_tw_affine_workspace_bytes(int64_t rows, int n_in, int n_out)
+{
+    if (rows <= 0 || n_in <= 0 || n_out <= 0 || n_in > MOST_WIDTH || n_out > MOST_WIDTH || rows > INT32_MAX) return 0;
+    const Layout l = layout_of(rows, n_in, n_out);
+    return l.w + l.x + l.parts + 256;  // (never 0 for what is valid)
+}
+
+int fpdt_tw_affine_fwd(const void* X, const void* W, const void* B, const void* R, void* Z, void* Y, int64_t rows, int n_in, int n_out, int act, int join,
+                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    clear_error();
+    if (!X || !W || !Y) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check_sizes(rows, n_in, n_out);
+    if (rc != TW_OK || (rc = check_kind(act, join)) != TW_OK) return rc;
+    if (join == FPDT_TW_JOIN_TIMES && !R) return fail(TW_INVALID, "JOIN_TIMES needs R");
+    for (const void* p : {X, W, B, R, (const void*)Z, (const void*)Y})
+        if (misaligned(p, 2)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (n_in % 8 == 0 && (misaligned(X, 16) || misaligned(W, 16))) return fail(TW_INVALID, "X and W must be 16-byte aligned where n_in is a multiple of 8");
+    const size_t need = fpdt_tw_affine_workspace_bytes(rows, n_in, n_out);
+    if (!workspace || workspace_bytes < need || misaligned(workspace, 256))
+        return fail(TW_WORKSPACE, "workspace NULL, misaligned or too small (%zu < %zu bytes)", workspace_bytes, need);
+    const size_t out = (size_t)rows * n_out * 2;
+    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, (size_t)n_in * n_out * 2, false}, {"B", B, (size_t)n_out * 2, false}, {"R", R, out, false},
+                        {"Z", Z, out, true}, {"Y", Y, out, true}, {"the workspace", workspace, need, true}};
+    const int same[][2] = {{3, 5}};
+    if ((rc = check_apart(args, 7, same, 1)) != TW_OK) return rc;
+
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Layout l = layout_of(rows, n_in, n_out);
+    char* ws = static_cast<char*>(workspace);
+    float* part = reinterpret_cast<float*>(ws + l.w + l.x);
+    Operand w = {static_cast<const uint16_t*>(W), n_in, n_out};
+    if (l.w) {
+        w.p = reinterpret_cast<const uint16_t*>(ws), w.ld = pitch_of(n_in);
+        realign(W, n_out, n_in, n_in, ws, w.ld, st);
+    }
+    const bool wide = all_wide(n_out, {B, R, Z, Y});
+    for (int64_t r0 = 0; r0 < rows; r0 += l.piece) {
+        const int m = (int)(rows - r0 < l.piece ? rows - r0 : l.piece);
+        const Plan plan = plan_of(m, n_in, n_out);
+        if (plan.u.tiles == 0) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+        Operand x = {static_cast<const uint16_t*>(X) + r0 * n_in, n_in, m};
+        if (l.x) {
+            realign(x.p, m, n_in, n_in, ws + l.w, w.ld, st);
+            x.p = reinterpret_cast<const uint16_t*>(ws + l.w), x.ld = w.ld;
+        }
+        const int64_t at = r0 * n_out;
+        const int64_t divided = plan.u.tiles - plan.u.whole, parts = divided * plan.u.splits;
+        const unsigned grid = 8 * ((unsigned)((plan.u.whole + 7) / 8) + (unsigned)((parts + 7) / 8));
+        by_act(act, [&](auto a) {
+            constexpr int ACT = decltype(a)::value;
+            const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), R ? static_cast<const uint16_t*>(R) + at : nullptr, Z ? static_cast<uint16_t*>(Z) + at : nullptr,
+                                          static_cast<uint16_t*>(Y) + at, join == FPDT_TW_JOIN_TIMES, wide};
+            by_tile(plan.wmt, plan.wnt, [&](auto wm, auto wn) {
+                affine_kernel<ACT, decltype(wm)::value, decltype(wn)::value><<<grid, NTHREAD, 0, st>>>(x, w, n_in, m, n_out, plan.u, part, behind);
+            });
+            const int tm = 64 * plan.wmt, tn = 64 * plan.wnt;
+            for (int64_t t0 = 0; plan.u.splits > 1 && t0 < divided; t0 += 65535)
+                affine_sum_kernel<ACT><<<dim3(tm * tn / 1024, (unsigned)(divided - t0 < 65535 ? divided - t0 : 65535)), 256, 0, st>>>(part, plan.u, (int)t0, tm, tn, m,
+                                                                                                                                      n_out, behind);
+        });
+    }
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+size_t fpdt_tw_affine_bwd_workspace_bytes(int64_t rows, int n_out, int experts)
+{
+    if (rows <= 0 || n_out <= 0 || experts <= 0 || n_out > MOST_WIDTH || rows > INT32_MAX || experts > MOST_EXPERTS) return 0;
+    const int64_t slice = slice_of(rows, n_out);
+    return al256((size_t)((rows + slice - 1) / slice + experts) * n_out * 4);
+}
+
+int fpdt_tw_affine_bwd(const void* Z, const void* R, const void* dY, void* dZ, void* dR, float* dB, int64_t rows, int n_out, int act, int join,
+                       const int32_t* offsets, int experts, void* workspace, size_t workspace_bytes, void* stream)
+{
+    clear_error();
+    if (!dY) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check_sizes(rows, 1, n_out);
+    if (rc != TW_OK || (rc = check_kind(act, join)) != TW_OK) return rc;
+    if (experts <= 0 || (!offsets && experts != 1)) return fail(TW_INVALID, "experts must be positive, and 1 without offsets");
+    if (experts > MOST_EXPERTS) return fail(TW_UNSUPPORTED, "experts=%d beyond %d", experts, MOST_EXPERTS);
+    const bool times = join == FPDT_TW_JOIN_TIMES, behind = times || act != FPDT_TW_ACT_NONE;
+    if (behind && (!Z || !dZ)) return fail(TW_INVALID, "an activation's or gate's backward needs Z and dZ");
+    if (times && !R) return fail(TW_INVALID, "JOIN_TIMES needs R");
+    if (!times && dR) return fail(TW_INVALID, "the gradient of an R that is added is dY: dR must be NULL");
+    if (!dZ && !dB) return fail(TW_INVALID, "nothing to compute: dZ and dB are NULL");
+    for (const void* p : {Z, R, dY, (const void*)dZ, (const void*)dR})
+        if (misaligned(p, 2)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (misaligned(dB, 4) || misaligned(offsets, 4)) return fail(TW_INVALID, "dB or offsets is not aligned to its elements");
+    const size_t need = dB ? fpdt_tw_affine_bwd_workspace_bytes(rows, n_out, experts) : 0, n = (size_t)rows * n_out * 2;
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 256)))
+        return fail(TW_WORKSPACE, "workspace NULL, misaligned or too small (%zu < %zu bytes)", workspace_bytes, need);
+    const Arg args[] = {{"Z", Z, n, false}, {"R", R, n, false}, {"dY", dY, n, false}, {"dZ", dZ, n, true}, {"dR", dR, n, true}, {"dB", dB, (size_t)experts * n_out * 4, true},
+                        {"offsets", offsets, (size_t)(experts + 1) * 4, false}, {"the workspace", need ? workspace : nullptr, need, true}};
+    const int same[][2] = {{0, 3}, {1, 3}, {2, 3}, {0, 4}, {1, 4}, {2, 4}};
+    if ((rc = check_apart(args, 8, same, 6)) != TW_OK) return rc;
+
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t slice = slice_of(rows, n_out), slices = (rows + slice - 1) / slice;
+    Backward b = {static_cast<const uint16_t*>(Z), static_cast<const uint16_t*>(R), static_cast<const uint16_t*>(dY), static_cast<uint16_t*>(dZ), static_cast<uint16_t*>(dR),
+                  dB ? static_cast<float*>(workspace) : nullptr, rows, n_out, experts, lanes_of(n_out), offsets, slice};
+    const dim3 grid((unsigned)((n_out + b.cols * 8 - 1) / (b.cols * 8)), (unsigned)slices);
+    by_act(act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        auto run = [&](auto t, auto w) { affine_bwd_kernel<ACT, decltype(t)::value, decltype(w)::value><<<grid, 256, 0, st>>>(b); };
+        typedef std::true_type Yes;
+        typedef std::false_type No;
+        if (times && n_out % 8 == 0) run(Yes(), Yes());
+        else if (times) run(Yes(), No());
+        else if (n_out % 8 == 0) run(No(), Yes());
+        else run(No(), No());
+    });
+    if (dB) affine_sums_kernel<<<dim3((unsigned)((n_out + 31) / 32), (unsigned)experts), 1024, 0, st>>>(b, dB);
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, const void* R, void* Z, void* Y, const int32_t* offsets, int64_t rows, int experts,
+                               int n_in, int n_out, int act, int join, void* stream)
+{
+    clear_error();
+    if (!X || !W || !Y || !offsets) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check_experts(rows, experts, n_in, n_out);
+    if (rc != TW_OK || (rc = check_kind(act, join)) != TW_OK) return rc;
+    if (join == FPDT_TW_JOIN_TIMES && !R) return fail(TW_INVALID, "JOIN_TIMES needs R");
+    for (const void* p : {B, R, (const void*)Z, (const void*)Y})
+        if (misaligned(p, 2)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (misaligned(X, 16) || misaligned(W, 16)) return fail(TW_INVALID, "X and W must be 16-byte aligned");
+    if (misaligned(offsets, 4)) return fail(TW_INVALID, "offsets is not aligned to its elements");
+    const size_t out = (size_t)rows * n_out * 2;
+    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, (size_t)experts * n_in * n_out * 2, false}, {"B", B, (size_t)experts * n_out * 2, false},
+                        {"R", R, out, false}, {"Z", Z, out, true}, {"Y", Y, out, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
+    const int same[][2] = {{3, 5}};
+    if ((rc = check_apart(args, 7, same, 1)) != TW_OK) return rc;
+    const GroupPlan plan = plan_groups(rows, experts, n_out, n_in);
+    if (plan.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+    const Groups g = {offsets, experts, (int)rows};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    by_act(act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y), join == FPDT_TW_JOIN_TIMES,
+                                      all_wide(n_out, {B, R, Z, Y})};
+        by_tile(plan.wmt, plan.wnt, [&](auto wm, auto wn) {
+            experts_affine_kernel<ACT, decltype(wm)::value, decltype(wn)::value>
+                <<<grid_of(plan.tiles), NTHREAD, 0, st>>>(static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
+        });
+    });
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+int fpdt_tw_experts_linear_bwd(const void* X, const void* W, const void* dY, void* dX, float* dW, const int32_t* offsets, int64_t rows, int experts, int n_in,
+                               int n_out, void* stream)
+{
+    clear_error();
+    if (!X || !W || !dY || !offsets) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check_experts(rows, experts, n_in, n_out);
+    if (rc != TW_OK) return rc;
+    if (misaligned(X, 16) || misaligned(W, 16) || misaligned(dY, 16)) return fail(TW_INVALID, "X, W and dY must be 16-byte aligned");
+    if (misaligned(dX, 2) || misaligned(dW, 4) || misaligned(offsets, 4)) return fail(TW_INVALID, "dX, dW or offsets is not aligned to its elements");
+    const size_t weights = (size_t)experts * n_in * n_out;
+    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, weights * 2, false}, {"dY", dY, (size_t)rows * n_out * 2, false},
+                        {"dX", dX, (size_t)rows * n_in * 2, true}, {"dW", dW, weights * 4, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
+    if ((rc = check_apart(args, 6, nullptr, 0)) != TW_OK) return rc;
+    const GroupPlan px = plan_groups(rows, experts, n_in, n_out), pw = plan_weights(rows, experts, n_in, n_out);
+    if (px.tiles > (int64_t)1 << 30 || pw.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+    const Groups g = {offsets, experts, (int)rows};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    auto t = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    if (dX)
+        by_tile(px.wmt, px.wnt, [&](auto wm, auto wn) {
+            experts_dx_kernel<decltype(wm)::value, decltype(wn)::value><<<grid_of(px.tiles), NTHREAD, 0, st>>>(t(dY), t(W), static_cast<uint16_t*>(dX), n_in, n_out, g);
+        });
+    if (dW)
+        by_tile(pw.wmt, pw.wnt, [&](auto wm, auto wn) {
+            experts_dw_kernel<decltype(wm)::value, decltype(wn)::value><<<grid_of(pw.tiles), NTHREAD, 0, st>>>(t(X), t(dY), dW, n_in, n_out, g);
+        });
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+}  // extern "C"

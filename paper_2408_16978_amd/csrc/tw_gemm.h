@@ -14,6 +14,9 @@ void* scratch(size_t bytes);
 // Does the product C [rows, cols] bf16 = A [rows, k] * .. read A where it is (and not a copy in scratch)?
 bool reads_in_place(const void* A, int64_t rows, int64_t k, const void* C, int64_t cols);
 
+// X [R, C], rows ld elements apart, copied to rows `pitch` elements apart (a multiple of 8; out 16-byte aligned): zeros behind C up to a multiple of 8.
+void realign(const void* X, int64_t R, int64_t C, int64_t ld, void* out, int64_t pitch, hipStream_t st);
+
 // C[M,N] (+)= sum_k Aop[m,k] * Bop[n,k], bf16 operands, fp32 accumulation.
 //   a_transposed = 0: A is stored [M,K] (leading dimension lda); 1: A is stored [K,M]
 //   b_transposed = 0: B is stored [N,K] (ldb);                   1: B is stored [K,N]

@@ -16,6 +16,8 @@ FPDT_TW_F32, FPDT_TW_BF16 = 0, 1
 FPDT_TW_ROPE_HALF, FPDT_TW_ROPE_INTERLEAVED = 0, 1
 FPDT_TW_ROPE_PLAIN, FPDT_TW_ROPE_LINEAR, FPDT_TW_ROPE_RAISED, FPDT_TW_ROPE_PARTS = range(4)
 FPDT_TW_RMSNORM, FPDT_TW_LAYERNORM = 0, 1
+FPDT_TW_ACT_NONE, FPDT_TW_ACT_GELU, FPDT_TW_ACT_SILU = 0, 1, 2
+FPDT_TW_JOIN_ADD, FPDT_TW_JOIN_TIMES = 0, 1
 FPDT_TW_ADAMW_ZERO_GRAD = 1 << 0
 FPDT_TW_STATE_BLOCK = 128  # elements that share an exponent byte of 8-bit states
 
@@ -62,6 +64,18 @@ def load():
     L.fpdt_tw_norm_bwd_workspace_bytes.argtypes = [i64, ci, ci]
     L.fpdt_tw_norm_bwd.restype = ci
     L.fpdt_tw_norm_bwd.argtypes = [vp] * 8 + [i64, ci, ci, ci, vp, sz, vp]
+    cu64 = ctypes.c_uint64
+    for name, args in (("affine_fwd", [vp] * 6 + [i64, ci, ci, ci, ci, vp, sz, vp]), ("affine_bwd", [vp] * 6 + [i64, ci, ci, ci, vp, ci, vp, sz, vp]),
+                       ("dropout_fwd", [vp] * 3 + [i64, i64, cd, cu64, i64, vp, ci, vp]), ("dropout_bwd", [vp] * 2 + [i64, i64, cd, cu64, i64, vp, ci, vp]),
+                       ("experts_sort", [vp] * 3 + [i64, ci, ci, vp, sz, vp]), ("experts_gather_fwd", [vp] * 3 + [i64, ci, ci, ci, vp]),
+                       ("experts_gather_bwd", [vp] * 4 + [i64, ci, ci, ci, vp]), ("experts_combine_fwd", [vp] * 5 + [i64, ci, ci, ci, vp]),
+                       ("experts_combine_bwd", [vp] * 6 + [i64, ci, ci, ci, vp]), ("experts_affine_fwd", [vp] * 7 + [i64, ci, ci, ci, ci, ci, vp]),
+                       ("experts_linear_bwd", [vp] * 6 + [i64, ci, ci, ci, vp])):
+        f = getattr(L, "fpdt_tw_" + name)
+        f.restype, f.argtypes = ci, args
+    for name, args in (("affine", [i64, ci, ci]), ("affine_bwd", [i64, ci, ci]), ("experts_sort", [i64, ci])):
+        f = getattr(L, "fpdt_tw_%s_workspace_bytes" % name)
+        f.restype, f.argtypes = sz, args
     L.fpdt_tw_grad_norm_workspace_bytes.restype = sz
     L.fpdt_tw_grad_norm_workspace_bytes.argtypes = [ci]
     L.fpdt_tw_grad_norm.restype = ci
@@ -279,6 +293,167 @@ def fpdt_tw_norm_bwd(S, W, stats, dY, dR, dX, dW, dB, kind=FPDT_TW_RMSNORM, work
     sums = [None if t is None else _expect(name, t, (hidden,), torch.float32, device) for name, t in (("dW", dW), ("dB", dB))]
     _check(load().fpdt_tw_norm_bwd(at[0], at[1], _stats(stats, rows, kind, device), *at[2:], *sums, rows, hidden, kind, code, *_room(workspace, device),
                                    _raw_stream(stream, device)))
+
+
+# ---- products with something behind them, dropout, experts
+def _sizes(*sizes):
+    for n in sizes:
+        if n >> _INT_BITS:
+            raise FpdtTwError(2, "sizes beyond the launch limits")
+
+
+def _half(name, t, shape, device):
+    return None if t is None else _expect(name, t, shape, torch.bfloat16, device)
+
+
+def fpdt_tw_affine_workspace_bytes(rows, n_in, n_out) -> int:
+    return 0 if (n_in | n_out) >> _INT_BITS else int(load().fpdt_tw_affine_workspace_bytes(rows, n_in, n_out))
+
+
+def fpdt_tw_affine_fwd(X, W, B, R, Z, Y, act=FPDT_TW_ACT_NONE, join=FPDT_TW_JOIN_ADD, workspace=None, stream=None):
+    """Y [rows, n_out] = act(X W^T + B) plus R (JOIN_ADD; R may be None) or times R (JOIN_TIMES); Z: what the activation is taken of, for the
+    backward, or None.  X [rows, n_in], W [n_out, n_in], B [n_out] or None; all bf16.  Y may be R itself."""
+    device, (rows, n_in), n_out = _current(X), X.shape, W.size(0)
+    _sizes(n_in, n_out)
+    out = (rows, n_out)
+    _check(load().fpdt_tw_affine_fwd(_half("X", X, X.shape, device), _half("W", W, (n_out, n_in), device), _half("B", B, (n_out,), device), _half("R", R, out, device),
+                                     _half("Z", Z, out, device), _half("Y", Y, out, device), rows, n_in, n_out, act, join, *_room(workspace, device),
+                                     _raw_stream(stream, device)))
+
+
+def _experts_of(offsets, device):
+    """(address, number of experts) of offsets, int32 [experts + 1]."""
+    if offsets is None:
+        return None, 1
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("fpdt_tw: offsets must be [experts + 1], got %s" % (tuple(offsets.shape),))
+    experts = offsets.numel() - 1
+    _sizes(experts)
+    return _expect("offsets", offsets, offsets.shape, torch.int32, device), experts
+
+
+def fpdt_tw_affine_bwd_workspace_bytes(rows, n_out, experts=1) -> int:
+    return 0 if (n_out | experts) >> _INT_BITS else int(load().fpdt_tw_affine_bwd_workspace_bytes(rows, n_out, experts))
+
+
+def fpdt_tw_affine_bwd(Z, R, dY, dZ, dR, dB, act=FPDT_TW_ACT_NONE, join=FPDT_TW_JOIN_ADD, offsets=None, workspace=None, stream=None):
+    """dZ (written) = dY act'(Z), times R with JOIN_TIMES, where dR (written, or None) = dY act(Z); dB (accumulated into, or None): fp32 [n_out], or
+    [experts, n_out] where offsets (of fpdt_tw_experts_sort) say whose rows are whose.  Then fpdt_tw_linear_bwd or fpdt_tw_experts_linear_bwd with dZ
+    for dY.  Z, R, dZ are None where they are not needed; dZ and dR may be Z, R or dY themselves."""
+    device, (rows, n_out) = _current(dY), dY.shape
+    _sizes(n_out)
+    place, experts = _experts_of(offsets, device)
+    z, r, dy, dz, dr = (_half(name, t, dY.shape, device) for name, t in (("Z", Z), ("R", R), ("dY", dY), ("dZ", dZ), ("dR", dR)))
+    db = None if dB is None else _expect("dB", dB, (n_out,) if offsets is None and dB.dim() == 1 else (experts, n_out), torch.float32, device)
+    _check(load().fpdt_tw_affine_bwd(z, r, dy, dz, dr, db, rows, n_out, act, join, place, experts, *_room(workspace, device), _raw_stream(stream, device)))
+
+
+def _dropout(call, tensors, p, seed, step, first, step_dev, stream):
+    X = tensors[0][1]
+    device, code = _current(X), _dtype_code(X)
+    at = [None if t is None else _expect(name, t, X.shape, X.dtype, device) for name, t in tensors]
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("fpdt_tw: seed must be in [0, 2^64), got %d" % seed)
+    if not (-1 << 63 <= step < 1 << 63 and 0 <= first < 1 << 62):
+        raise FpdtTwError(2, "step beyond 64 bits, or first beyond [0, 2^62)")
+    _check(call(*at, X.numel(), first, p, seed, step, None if step_dev is None else _expect("step_dev", step_dev, step_dev.shape if step_dev.numel() == 1 else (1,), torch.int64, device),
+                code, _raw_stream(stream, device)))
+
+
+def fpdt_tw_dropout_fwd(X, R, Y, p, seed, step=0, first=0, step_dev=None, stream=None):
+    """Y = X dropped with probability p (to a 65536th) and scaled, plus R (or None).  The choice depends on seed (a number of its own for each layer),
+    step and the element's number, from `first` on: a chunk of a sequence gives its first element's number in the whole.  step_dev: None, or one int64
+    on the device in place of step.  Y may be X or R itself."""
+    _dropout(load().fpdt_tw_dropout_fwd, (("X", X), ("R", R), ("Y", Y)), p, seed, step, first, step_dev, stream)
+
+
+def fpdt_tw_dropout_bwd(dY, dX, p, seed, step=0, first=0, step_dev=None, stream=None):
+    """dX: dY where the forward of the same seed, step and first kept its element, scaled; 0 elsewhere.  dX may be dY itself."""
+    _dropout(load().fpdt_tw_dropout_bwd, (("dY", dY), ("dX", dX)), p, seed, step, first, step_dev, stream)
+
+
+def fpdt_tw_experts_sort_workspace_bytes(assignments, experts) -> int:
+    return 0 if experts >> _INT_BITS else int(load().fpdt_tw_experts_sort_workspace_bytes(assignments, experts))
+
+
+def fpdt_tw_experts_sort(expert, offsets, place, workspace, stream=None):
+    """offsets [experts + 1]: where each expert's rows begin, and all of them end; place [rows, top]: the row of each assignment of expert
+    [rows, top], or -1 where that is no expert's number.  All int32.  In the order of experts, then tokens."""
+    device, (rows, top) = _current(expert), expert.shape
+    _sizes(top)
+    at, experts = _experts_of(offsets, device)
+    _check(load().fpdt_tw_experts_sort(_expect("expert", expert, expert.shape, torch.int32, device), at, _expect("place", place, expert.shape, torch.int32, device),
+                                       rows, top, experts, *_room(workspace, device), _raw_stream(stream, device)))
+
+
+def _routed(device, place, one, wide, weights=()):
+    """Checks of tokens [rows, hidden] (`one`) and their copies [rows top, hidden] (`wide`): addresses of place, of `one`, `wide` and `weights` in that order, and the sizes."""
+    if place.dim() != 2:
+        raise ValueError("fpdt_tw: place must be [rows, top], got %s" % (tuple(place.shape),))
+    (rows, top), some = place.shape, next(t for _, t in one + wide if t is not None)
+    hidden, dtype, code = some.size(-1), some.dtype, _dtype_code(some)
+    _sizes(top, hidden)
+    at = [_expect("place", place, place.shape, torch.int32, device)]
+    at += [None if t is None else _expect(name, t, (rows, hidden), dtype, device) for name, t in one]
+    at += [None if t is None else _expect(name, t, (rows * top, hidden), dtype, device) for name, t in wide]
+    at += [None if t is None else _expect(name, t, (rows, top), torch.float32, device) for name, t in weights]
+    return at, (rows, top, hidden, code)
+
+
+def fpdt_tw_experts_gather_fwd(X, place, Xs, stream=None):
+    """Xs [rows top, hidden]: the tokens of X [rows, hidden] at their places; rows without an assignment are left as they were."""
+    device = _current(X)
+    (p, x, xs), sizes = _routed(device, place, (("X", X),), (("Xs", Xs),))
+    _check(load().fpdt_tw_experts_gather_fwd(x, p, xs, *sizes, _raw_stream(stream, device)))
+
+
+def fpdt_tw_experts_gather_bwd(dXs, place, R, dX, stream=None):
+    """dX [rows, hidden]: sums of the gradients dXs [rows top, hidden] over each token's places, plus R (or None; dX may be R itself)."""
+    device = _current(dXs)
+    (p, r, dx, dxs), sizes = _routed(device, place, (("R", R), ("dX", dX)), (("dXs", dXs),))
+    _check(load().fpdt_tw_experts_gather_bwd(dxs, p, r, dx, *sizes, _raw_stream(stream, device)))
+
+
+def fpdt_tw_experts_combine_fwd(Ys, weight, place, R, Y, stream=None):
+    """Y [rows, hidden]: sums of Ys [rows top, hidden] over each token's places, weighted (fp32 [rows, top]), plus R (or None; Y may be R itself)."""
+    device = _current(Ys)
+    (p, r, y, ys, w), sizes = _routed(device, place, (("R", R), ("Y", Y)), (("Ys", Ys),), (("weight", weight),))
+    _check(load().fpdt_tw_experts_combine_fwd(ys, w, p, r, y, *sizes, _raw_stream(stream, device)))
+
+
+def fpdt_tw_experts_combine_bwd(Ys, weight, place, dY, dYs, dweight, stream=None):
+    """dYs (written, or None; rows without an assignment are left as they were): each place's token of dY, weighted; dweight (written, or None): the products
+    of dY with each place's row of Ys.  dYs may be Ys itself."""
+    device = _current(dY)
+    (p, dy, ys, dys, w, dw), sizes = _routed(device, place, (("dY", dY),), (("Ys", Ys), ("dYs", dYs)), (("weight", weight), ("dweight", dweight)))
+    _check(load().fpdt_tw_experts_combine_bwd(ys, w, p, dy, dys, dw, *sizes, _raw_stream(stream, device)))
+
+
+def fpdt_tw_experts_affine_fwd(X, W, B, R, Z, Y, offsets, act=FPDT_TW_ACT_NONE, join=FPDT_TW_JOIN_ADD, stream=None):
+    """fpdt_tw_affine_fwd for the rows of each expert (offsets of fpdt_tw_experts_sort) with its own W [experts, n_out, n_in] and B [experts, n_out] (or None)."""
+    device, (rows, n_in) = _current(X), X.shape
+    at, experts = _experts_of(offsets, device)
+    if W.dim() != 3:
+        raise ValueError("fpdt_tw: W must be [experts, n_out, n_in], got %s" % (tuple(W.shape),))
+    n_out = W.size(1)
+    _sizes(n_in, n_out)
+    out = (rows, n_out)
+    _check(load().fpdt_tw_experts_affine_fwd(_half("X", X, X.shape, device), _half("W", W, (experts, n_out, n_in), device), _half("B", B, (experts, n_out), device),
+                                             _half("R", R, out, device), _half("Z", Z, out, device), _half("Y", Y, out, device), at, rows, experts, n_in, n_out, act, join,
+                                             _raw_stream(stream, device)))
+
+
+def fpdt_tw_experts_linear_bwd(X, W, dY, dX, dW, offsets, stream=None):
+    """dX (bf16, written, or None) = dY W of each row's expert;  dW (fp32 [experts, n_out, n_in], accumulated into, or None) += dY^T X over its rows."""
+    device, (rows, n_in) = _current(X), X.shape
+    at, experts = _experts_of(offsets, device)
+    if W.dim() != 3:
+        raise ValueError("fpdt_tw: W must be [experts, n_out, n_in], got %s" % (tuple(W.shape),))
+    n_out = W.size(1)
+    _sizes(n_in, n_out)
+    _check(load().fpdt_tw_experts_linear_bwd(_half("X", X, X.shape, device), _half("W", W, (experts, n_out, n_in), device), _half("dY", dY, (rows, n_out), device),
+                                             _half("dX", dX, X.shape, device), None if dW is None else _expect("dW", dW, W.shape, torch.float32, device), at, rows,
+                                             experts, n_in, n_out, _raw_stream(stream, device)))
 
 
 class _Param(ctypes.Structure):
