@@ -26,12 +26,19 @@ __device__ __forceinline__ float normal_below(float a, float e)
 __device__ __forceinline__ float exp_half_square(float a) { return __builtin_amdgcn_exp2f(a * -0.72134752044448170f * a); }
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f)); }
 
-// x Phi(x) = max(x, 0) - |x| Phi(-|x|): infinities keep their value (20 Phi(-20) is nothing next to any of them), NaN stays NaN.
+// x Phi(x) = max(x, 0) - |x| Phi(-|x|): infinities keep their value (20 Phi(-20) is nothing next to any of them), NaN stays NaN.  (fmaxf would be two
+// instructions.)
+__device__ __forceinline__ float gelu_of(float x, float a, float below)
+{
+    float top;
+    asm("v_max_f32 %0, 0, %1" : "=v"(top) : "v"(x));
+    return fmaf(-__builtin_amdgcn_fmed3f(a, 0.f, 20.f), below, top);
+}
 template <int ACT> __device__ __forceinline__ float act_of(float x)
 {
     if constexpr (ACT == FPDT_TW_ACT_GELU) {
         const float a = fabsf(x);
-        return fmaf(-fminf(a, 20.f), normal_below(a, exp_half_square(a)), fmaxf(x, 0.f));
+        return gelu_of(x, a, normal_below(a, exp_half_square(a)));
     } else if constexpr (ACT == FPDT_TW_ACT_SILU) {
         return x * logistic(x);
     } else {
@@ -44,7 +51,7 @@ template <int ACT> __device__ __forceinline__ float slope_of(float x, float& y)
 {
     if constexpr (ACT == FPDT_TW_ACT_GELU) {
         const float a = fabsf(x), e = exp_half_square(a), below = normal_below(a, e);
-        y = fmaf(-fminf(a, 20.f), below, fmaxf(x, 0.f));
+        y = gelu_of(x, a, below);
         return fmaf(x * 0.3989422804014327f, e, x > 0.f ? 1.f - below : below);
     } else if constexpr (ACT == FPDT_TW_ACT_SILU) {
         const float s = logistic(x);

@@ -422,11 +422,34 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
             copied = 1;
         }
     }
+    // What joins a whole tile behind its product is requested in front of the last two stages, as much of it as there are registers for, and
+    // comes under their MFMAs: JOIN_LOADS loads, each issued (no condition), and held in front of those stages by the statement behind them,
+    // so that the wait for the last stage's copies can count them.
+    const int mt = tile_m * (64 * WMT), nt = tile_n * (64 * WNT);
+    constexpr int NA = NI / 2, JOIN_ROWS = Behind::any ? (MI < 4 ? MI : 4) : 0, JOIN_LOADS = JOIN_ROWS * NA;
+    const int b_row = mt + wm * (32 * WMT) + (lane & 15), b_col = nt + wn * (32 * WNT) + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);  // as in store_bf16
+    const int64_t b_at = (int64_t)b_row * ldc + b_col;
+    u32x4 joins[Behind::any ? MI : 1][NA];
+    bool early = false;
+    if constexpr (Behind::any) {
+        early = !is_part && behind.R && behind.wide && mt + 64 * WMT <= M && nt + 64 * WNT <= N;
+        if (early) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < JOIN_ROWS; ++i)
+#pragma unroll
+                for (int k = 0; k < NA; ++k) joins[i][k] = *reinterpret_cast<const u32x4*>(behind.R + b_at + (int64_t)(16 * i) * ldc + 32 * k);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
     // the last two
     int left = total < 2 ? total : 2;
     do {
         half_stage(Ks0{}, std::false_type{}, cur_a, cur_b, 0u, 0u);
-        fpdt::wait_vmem_at_most<0>();
+        if (!early) fpdt::wait_vmem_at_most<0>();
+        else if (left == 2) fpdt::wait_vmem_at_most<JOIN_LOADS>();
         if (left == 2 && k_left > 0) clear_tail(nxt_a, nxt_b);
         fpdt::barrier_no_fence();
         __builtin_amdgcn_sched_barrier(0);
@@ -534,30 +557,39 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
         store_f32(part_of(TILE_ELEMS), 64 * WNT, 64 * WMT, 64 * WNT, std::false_type{}, std::true_type{});
         return;
     }
-    const int mt = tile_m * (64 * WMT), nt = tile_n * (64 * WNT);
     if constexpr (Behind::any) {
-        // The tile goes through `behind` in fp32, as it lies in store_bf16: eight columns of a row per lane and access.  What joins it is
-        // requested a row of accumulator tiles ahead, as old values are.  (behind.Y, not Cout: it may be what joins.)
-        constexpr int NA = NI / 2;
-        const int g = lane >> 4, row = mt + mw + (lane & 15), col = nt + nw + 16 * (g & 1) + 8 * (g >> 1);
-        auto store_behind = [&](auto whole_tag) {
-            constexpr bool WHOLE = decltype(whole_tag)::value;
-            auto in = [&](int i, int k) { return WHOLE || (row + 16 * i < M && col + 32 * k < N); };
-            const int64_t at0 = (int64_t)row * ldc + col;
-            u32x4 bias[NA] = {}, joins[2][NA] = {};
+        // The tile goes through `behind` in fp32, as it lies in store_bf16: eight columns of a row per lane and access.  Where nothing joins it, past the
+        // caches, which keep the operands then (us, through them -> past them: 16384 x 2560 x 10240 with bias, GELU and Z 729 -> 699, 16384 x 4096 x
+        // 14336 without any 1294 -> 1270; with a gate and Z 732 -> 752 and 1433 -> 1505).  (behind.Y, not Cout: it may be what joins.)
+        auto store_behind = [&](auto whole_tag, auto joins_tag) {
+            constexpr bool WHOLE = decltype(whole_tag)::value, JOINS = decltype(joins_tag)::value;
+            auto in = [&](int i, int k) { return WHOLE || (b_row + 16 * i < M && b_col + 32 * k < N); };
+            auto put = [&](uint16_t* p, const float (&v)[8]) {
+                const u32x4 x = pack_bf16(floatx4{v[0], v[1], v[2], v[3]}, floatx4{v[4], v[5], v[6], v[7]});
+                if (JOINS) *reinterpret_cast<u32x4*>(p) = x;
+                else __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+            };
+            u32x4 bias[NA] = {};
             if (behind.B)
 #pragma unroll
                 for (int k = 0; k < NA; ++k)
-                    if (WHOLE || col + 32 * k < N) bias[k] = *reinterpret_cast<const u32x4*>(behind.B + col + 32 * k);
-            auto request = [&](int i) {
+                    if (WHOLE || b_col + 32 * k < N) bias[k] = *reinterpret_cast<const u32x4*>(behind.B + b_col + 32 * k);
+            if (JOINS)
 #pragma unroll
-                for (int k = 0; k < NA; ++k)
-                    if (in(i, k)) joins[i & 1][k] = *reinterpret_cast<const u32x4*>(behind.R + at0 + (int64_t)(16 * i) * ldc + 32 * k);
-            };
-            if (behind.R) request(0);
+                for (int i = WHOLE ? JOIN_ROWS : 0; i < MI; ++i)
+#pragma unroll
+                    for (int k = 0; k < NA; ++k)
+                        if (in(i, k)) joins[i][k] = *reinterpret_cast<const u32x4*>(behind.R + b_at + (int64_t)(16 * i) * ldc + 32 * k);
+            // All of it is here before the first store: a wait for a load behind stores that may or may not have been made is a wait for those, too.
+#pragma unroll
+            for (int k = 0; k < NA; ++k) asm volatile("" : "+v"(bias[k]));
+            if (JOINS)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int k = 0; k < NA; ++k) asm volatile("" : "+v"(joins[i][k]));
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                if (behind.R && i + 1 < MI) request(i + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int k = 0; k < NA; ++k) {
@@ -569,20 +601,30 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
                         v[r] = __uint_as_float(xy[0]) + half_of(bias[k], r);
                         v[4 + r] = __uint_as_float(xy[1]) + half_of(bias[k], 4 + r);
                     }
-                    const int64_t at = at0 + (int64_t)(16 * i) * ldc + 32 * k;
-                    if (behind.Z && in(i, k)) *reinterpret_cast<u32x4*>(behind.Z + at) = pack_bf16(floatx4{v[0], v[1], v[2], v[3]}, floatx4{v[4], v[5], v[6], v[7]});
+                    const int64_t at = b_at + (int64_t)(16 * i) * ldc + 32 * k;
+                    if (behind.Z && in(i, k)) put(behind.Z + at, v);
 #pragma unroll
                     for (int r = 0; r < 8; ++r) v[r] = behind.act(v[r]);
-                    if (behind.R)
+                    if (JOINS) {
+                        if (behind.times) {
 #pragma unroll
-                        for (int r = 0; r < 8; ++r) v[r] = behind.times ? v[r] * half_of(joins[i & 1][k], r) : v[r] + half_of(joins[i & 1][k], r);
-                    if (in(i, k)) *reinterpret_cast<u32x4*>(behind.Y + at) = pack_bf16(floatx4{v[0], v[1], v[2], v[3]}, floatx4{v[4], v[5], v[6], v[7]});
+                            for (int r = 0; r < 8; ++r) v[r] *= half_of(joins[i][k], r);
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) v[r] += half_of(joins[i][k], r);
+                        }
+                    }
+                    if (in(i, k)) put(behind.Y + at, v);
                 }
             }
         };
         if (behind.wide) {
-            if (mt + 64 * WMT <= M && nt + 64 * WNT <= N) store_behind(std::true_type{});
-            else store_behind(std::false_type{});
+            auto store = [&](auto whole_tag) {
+                if (behind.R) store_behind(whole_tag, std::true_type{});
+                else store_behind(whole_tag, std::false_type{});
+            };
+            if (mt + 64 * WMT <= M && nt + 64 * WNT <= N) store(std::true_type{});
+            else store(std::false_type{});
             return;
         }
         // rows that do not come in pieces of 16 bytes: through LDS, one element per lane and access, as below
