@@ -1,53 +1,30 @@
-// Products with bias, activation and residual or gate behind them, dense and for the rows of many experts, and what their backward
-// needs (include/fpdt_tokenwise.h: fpdt_tw_affine_*, fpdt_tw_experts_affine_fwd, fpdt_tw_experts_linear_bwd).
+// Products with bias, activation and residual or gate behind them, and the backward of what is behind them (include/fpdt_tokenwise.h:
+// fpdt_tw_affine_*).
 //
-//     z = x W^T + b,   y = act(z) + r  or  act(z) r                          (W, b: of the row's expert)
+//     z = x W^T + b,   y = act(z) + r  or  act(z) r
 //     dz = dy act'(z) (r),   dr = dy act(z),   db += sum_rows dz
-//     dx = dy W,   dW += dy^T x                                              (for each expert's rows)
 //
-// The products run the tile loop of tw_gemm_tile.h.  An expert's rows are neighbours, from offsets[e] on; offsets are known to the
-// device alone, so a launch has as many workgroups as the rows could need, and each finds its expert and tile from them.
+// The products run the tile loop of tw_gemm_tile.h, which hands finished tiles to an Epilogue.
 #include <cmath>
 #include <type_traits>
 
-#include "../../include/fpdt_tokenwise.h"
-#include "tw_act.h"
-#include "tw_common.h"
+#include "tw_affine.h"
 #include "tw_gemm.h"
-#include "tw_gemm_tile.h"
 
 namespace fpdt_tw {
 namespace {
 
-constexpr int MOST_EXPERTS = 1024;
-constexpr int MOST_WIDTH = 1 << 22;              // a lane's offset within a tile is kept in 32 bits
 constexpr int64_t MOST_ROWS = (int64_t)1 << 24;  // of one dense product
-
-// What is done behind a product, in fp32.  Pointers are to the first of the product's rows (B: columns).
-template <int ACT> struct Epilogue {
-    static constexpr bool any = true;
-    const uint16_t *B, *R;
-    uint16_t *Z, *Y;
-    bool times;  // R multiplies the activation, otherwise it is added to it
-    bool wide;   // rows come in aligned pieces of 16 bytes in all of them
-    __device__ __forceinline__ float act(float z) const { return act_of<ACT>(z); }
-    __device__ __forceinline__ void one(float z, int64_t at) const
-    {
-        if (Z) Z[at] = from_float<uint16_t>(z);
-        float y = act(z);
-        if (R) y = times ? y * to_float(R[at]) : y + to_float(R[at]);
-        Y[at] = from_float<uint16_t>(y);
-    }
-};
 
 template <int ACT, int WMT, int WNT>
 __global__ __launch_bounds__(NTHREAD, 1) void affine_kernel(Operand A, Operand B, int K, int M, int N, Units u, float* part, Epilogue<ACT> behind)
 {
+    __shared__ __attribute__((aligned(256))) u32x4 ring[ring_bytes(WMT, WNT) / 16];
     Unit at;
     if (!find_unit(u, at)) return;
     const int unit_stages = at.is_part ? u.split_stages : K / STAGE_K;
     auto part_of = [&](size_t elems) { return part + ((size_t)at.split * (unsigned)(u.tiles - u.whole) + (at.id - (unsigned)u.whole)) * elems; };
-    product_tile<false, false, false, false, WMT, WNT>(A, B, K, nullptr, N, M, N, at.tile_m, at.tile_n, (int)at.split * unit_stages, unit_stages, at.is_part, part_of, behind);
+    product_tile<false, false, false, false, WMT, WNT>(ring, A, B, K, nullptr, N, M, N, at.tile_m, at.tile_n, (int)at.split * unit_stages, unit_stages, at.is_part, part_of, behind);
 }
 
 // The divided tiles of a product, as tw_split_sum_kernel adds them, and what is behind it.
@@ -88,103 +65,6 @@ __global__ __launch_bounds__(256) void affine_sum_kernel(const float* part, Unit
     } else {
         for (int r = 0; r < 4 && n + r < N; ++r) behind.one(v[r] + (behind.B ? to_float(behind.B[n + r]) : 0.f), c + r);
     }
-}
-
-// ---- experts ------------------------------------------------------------------------------
-// Where expert e's rows begin and end, whatever the offsets say within the rows that there are.
-__device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int rows)
-{
-    const int o = offsets[e];
-    return o < 0 ? 0 : o < rows ? o : rows;
-}
-
-struct Groups {
-    const int32_t* offsets;
-    int experts, rows;
-};
-
-// Tile number `turn` of this XCD's share, of all experts' tiles of tm rows in their order: the expert, its rows, and the tile among its own.
-struct GroupTile {
-    int expert, first, rows, tile_m, tile_n;
-};
-__device__ __forceinline__ bool find_group(const Groups& g, int tm, unsigned tiles_n, GroupTile& at)
-{
-    // a lane counts the tile rows of `per` neighbouring experts
-    const int lane = threadIdx.x & 63, per = (g.experts + 63) / 64, e0 = lane * per;
-    auto rows_of = [&](int e) {
-        const int n = offset_of(g.offsets, e + 1, g.rows) - offset_of(g.offsets, e, g.rows);
-        return n > 0 ? n : 0;
-    };
-    unsigned mine = 0;
-#pragma unroll 4
-    for (int i = 0; i < per; ++i)
-        if (e0 + i < g.experts) mine += (unsigned)(rows_of(e0 + i) + tm - 1) / (unsigned)tm;
-    unsigned upto = mine;  // those of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const unsigned v = __shfl_up(upto, d, 64);
-        if (lane >= d) upto += v;
-    }
-    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * tiles_n;
-    const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8, run = (total + 7) / 8, id = xcd * run + turn;
-    if (turn >= run || id >= total) return false;  // whole workgroup, before any barrier
-    const int owner = __builtin_ctzll(__ballot(upto * tiles_n > id));
-    unsigned base = (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), owner), tiles = 0;
-    int e = owner * per;
-    for (;; ++e) {
-        tiles = (unsigned)(rows_of(e) + tm - 1) / (unsigned)tm;
-        if ((base + tiles) * tiles_n > id || e + 1 >= g.experts) break;
-        base += tiles;
-    }
-    if (id - base * tiles_n >= tiles * tiles_n) return false;  // (offsets that do not ascend)
-    at.expert = (int)fpdt::uniform((unsigned)e);
-    at.first = (int)fpdt::uniform((unsigned)offset_of(g.offsets, e, g.rows));
-    at.rows = (int)fpdt::uniform((unsigned)rows_of(e));
-    tile_of(fpdt::uniform(id - base * tiles_n), fpdt::uniform(tiles), tiles_n, at.tile_m, at.tile_n);
-    return true;
-}
-
-template <int ACT, int WMT, int WNT>
-__global__ __launch_bounds__(NTHREAD, 1) void experts_affine_kernel(const uint16_t* X, const uint16_t* W, int n_in, int n_out, Groups g, Epilogue<ACT> behind)
-{
-    GroupTile t;
-    if (!find_group(g, 64 * WMT, ((unsigned)n_out + 64 * WNT - 1) / (64 * WNT), t)) return;
-    const int64_t out = (int64_t)t.first * n_out;
-    const Operand a = {X + (int64_t)t.first * n_in, n_in, t.rows}, b = {W + (int64_t)t.expert * n_out * n_in, n_in, n_out};
-    if (behind.B) behind.B += (int64_t)t.expert * n_out;
-    if (behind.R) behind.R += out;
-    if (behind.Z) behind.Z += out;
-    behind.Y += out;
-    product_tile<false, false, false, false, WMT, WNT>(a, b, n_in, nullptr, n_out, t.rows, n_out, t.tile_m, t.tile_n, 0, n_in / STAGE_K, false,
-                                                       [](size_t) { return (float*)nullptr; }, behind);
-}
-
-// dX of an expert's rows = dY W
-template <int WMT, int WNT>
-__global__ __launch_bounds__(NTHREAD, 1) void experts_dx_kernel(const uint16_t* dY, const uint16_t* W, uint16_t* dX, int n_in, int n_out, Groups g)
-{
-    GroupTile t;
-    if (!find_group(g, 64 * WMT, ((unsigned)n_in + 64 * WNT - 1) / (64 * WNT), t)) return;
-    const Operand a = {dY + (int64_t)t.first * n_out, n_out, t.rows}, b = {W + (int64_t)t.expert * n_out * n_in, n_in, n_in};
-    product_tile<false, true, false, false, WMT, WNT>(a, b, n_out, dX + (int64_t)t.first * n_in, n_in, t.rows, n_in, t.tile_m, t.tile_n, 0, n_out / STAGE_K, false,
-                                                      [](size_t) { return (float*)nullptr; }, Nothing());
-}
-
-// dW of an expert += dY^T X over its rows
-template <int WMT, int WNT>
-__global__ __launch_bounds__(NTHREAD, 1) void experts_dw_kernel(const uint16_t* X, const uint16_t* dY, float* dW, int n_in, int n_out, Groups g)
-{
-    const unsigned tiles_n = ((unsigned)n_in + 64 * WNT - 1) / (64 * WNT), tiles_m = ((unsigned)n_out + 64 * WMT - 1) / (64 * WMT);
-    const unsigned total = tiles_m * tiles_n * (unsigned)g.experts, run = (total + 7) / 8, xcd = blockIdx.x % 8, turn = blockIdx.x / 8, id = xcd * run + turn;
-    if (turn >= run || id >= total) return;
-    const unsigned e = id / (tiles_m * tiles_n);
-    const int first = (int)fpdt::uniform((unsigned)offset_of(g.offsets, (int)e, g.rows)), last = (int)fpdt::uniform((unsigned)offset_of(g.offsets, (int)e + 1, g.rows));
-    if (last <= first) return;
-    int tile_m, tile_n;
-    tile_of(id - e * (tiles_m * tiles_n), tiles_m, tiles_n, tile_m, tile_n);
-    const Operand a = {dY + (int64_t)first * n_out, n_out, n_out}, b = {X + (int64_t)first * n_in, n_in, n_in};
-    product_tile<true, true, true, true, WMT, WNT>(a, b, last - first, dW + (int64_t)e * n_out * n_in, n_in, n_out, n_in, tile_m, tile_n, 0, (last - first) / STAGE_K, false,
-                                                   [](size_t) { return (float*)nullptr; }, Nothing());
 }
 
 // ---- backward of what is behind a product -------------------------------------------------
@@ -329,56 +209,6 @@ __global__ __launch_bounds__(1024) void affine_sums_kernel(Backward b, float* dB
 // ---- host side ----------------------------------------------------------------------------
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// f(Int<act>) for an activation that was checked
-template <class F> void by_act(int act, F f)
-{
-    if (act == FPDT_TW_ACT_GELU) f(Int<FPDT_TW_ACT_GELU>());
-    else if (act == FPDT_TW_ACT_SILU) f(Int<FPDT_TW_ACT_SILU>());
-    else f(Int<FPDT_TW_ACT_NONE>());
-}
-// f(Int<WMT>, Int<WNT>) for the tiles that plans have
-template <class F> void by_tile(int wmt, int wnt, F f)
-{
-    if (wnt == 2) f(Int<2>(), Int<2>());
-    else if (wmt == 4) f(Int<4>(), Int<4>());
-    else if (wmt == 3) f(Int<3>(), Int<4>());
-    else if (wmt == 2) f(Int<2>(), Int<4>());
-    else f(Int<1>(), Int<4>());
-}
-
-int check_sizes(int64_t rows, int n_in, int n_out)
-{
-    if (rows <= 0 || n_in <= 0 || n_out <= 0) return fail(TW_INVALID, "rows, n_in and n_out must be positive");
-    if (n_in > MOST_WIDTH || n_out > MOST_WIDTH || rows > INT32_MAX) return fail(TW_UNSUPPORTED, "sizes beyond the launch limits");
-    return TW_OK;
-}
-int check_kind(int act, int join)
-{
-    if (act < FPDT_TW_ACT_NONE || act > FPDT_TW_ACT_SILU) return fail(TW_INVALID, "unknown activation %d", act);
-    if (join != FPDT_TW_JOIN_ADD && join != FPDT_TW_JOIN_TIMES) return fail(TW_INVALID, "unknown join %d", join);
-    return TW_OK;
-}
-
-// A tensor of a call: what it is called, its bytes, whether it is written.
-struct Arg {
-    const char* name;
-    const void* p;
-    size_t bytes;
-    bool written;
-};
-// Two of them that overlap, one at least written, are refused, but for `same`: pairs that may be one tensor (not a part of it).
-int check_apart(const Arg* a, int n, const int (*same)[2], int nsame)
-{
-    for (int i = 0; i < n; ++i)
-        for (int j = i + 1; j < n; ++j) {
-            if (!a[i].p || !a[j].p || !(a[i].written || a[j].written) || !ranges_meet(a[i].p, a[i].bytes, a[j].p, a[j].bytes)) continue;
-            bool may = false;
-            for (int k = 0; k < nsame; ++k) may = may || (a[i].p == a[j].p && same[k][0] == i && same[k][1] == j);
-            if (!may) return fail(TW_INVALID, "%s and %s overlap", a[i].name, a[j].name);
-        }
-    return TW_OK;
-}
-
 // The dense product: its copies and partial sums in the workspace.  Copies are made where rows are no multiple of 16 bytes, of X for
 // PIECE rows at a time.
 constexpr int64_t PIECE = 32768;
@@ -401,58 +231,6 @@ Layout layout_of(int64_t rows, int n_in, int n_out)
             if (b > l.parts) l.parts = b;
         }
     return l;
-}
-
-bool all_wide(int n, std::initializer_list<const void*> every)
-{
-    for (const void* p : every)
-        if (misaligned(p, 16)) return false;
-    return n % 8 == 0;
-}
-
-// Tiles for experts' products of about rows / experts rows each: the cheapest by launch_cost's measure, without divided tiles.
-struct GroupPlan {
-    int wmt, wnt;
-    int64_t tiles;  // at most, whatever the offsets
-};
-GroupPlan plan_groups(int64_t rows, int experts, int N, int K)
-{
-    static const int shapes[][2] = {{4, 4}, {3, 4}, {2, 4}, {1, 4}, {2, 2}};
-    GroupPlan best = {4, 4, 0};
-    double best_cost = 0;
-    const int64_t busy = rows < experts ? rows : experts;
-    for (const auto& sh : shapes) {
-        const int64_t tiles_n = (N + 64 * sh[1] - 1) / (64 * sh[1]), tm = 64 * sh[0], each = ((rows + busy - 1) / busy + tm - 1) / tm, tiles = each * busy * tiles_n;
-        const int slots = sh[0] * sh[1] <= 4 ? 512 : 256;
-        const double c = launch_cost(sh[0], sh[1], (double)(tiles / slots * slots), (double)(tiles % slots), 1, (K < SK ? SK : K) / SK);
-        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], (rows / tm + busy) * tiles_n}, best_cost = c;
-    }
-    return best;
-}
-GroupPlan plan_weights(int64_t rows, int experts, int n_in, int n_out)
-{
-    static const int shapes[][2] = {{4, 4}, {3, 4}, {2, 4}, {1, 4}, {2, 2}};
-    GroupPlan best = {4, 4, 0};
-    double best_cost = 0;
-    const int64_t busy = rows < experts ? rows : experts, K = (rows + busy - 1) / busy;
-    for (const auto& sh : shapes) {
-        const int64_t each = (int64_t)((n_in + 64 * sh[1] - 1) / (64 * sh[1])) * ((n_out + 64 * sh[0] - 1) / (64 * sh[0])), tiles = each * busy;
-        const int slots = sh[0] * sh[1] <= 4 ? 512 : 256;
-        const double c = launch_cost(sh[0], sh[1], (double)(tiles / slots * slots), (double)(tiles % slots), 1, (int)((K < SK ? SK : K) / SK));
-        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], each * experts}, best_cost = c;
-    }
-    return best;
-}
-unsigned grid_of(int64_t tiles) { return 8u * (unsigned)((tiles + 7) / 8); }
-
-int check_experts(int64_t rows, int experts, int n_in, int n_out)
-{
-    int rc = check_sizes(rows, n_in, n_out);
-    if (rc != TW_OK) return rc;
-    if (experts <= 0) return fail(TW_INVALID, "experts must be positive");
-    if (experts > MOST_EXPERTS) return fail(TW_UNSUPPORTED, "experts=%d beyond %d", experts, MOST_EXPERTS);
-    if (n_in % 8 || n_out % 8) return fail(TW_UNSUPPORTED, "n_in=%d and n_out=%d of experts must be multiples of 8", n_in, n_out);
-    return TW_OK;
 }
 
 int lanes_of(int n)
@@ -590,70 +368,6 @@ int fpdt_tw_affine_bwd(const void* Z, const void* R, const void* dY, void* dZ, v
         else run(No(), No());
     });
     if (dB) affine_sums_kernel<<<dim3((unsigned)((n_out + 31) / 32), (unsigned)experts), 1024, 0, st>>>(b, dB);
-    HIP_TRY(hipGetLastError());
-    return TW_OK;
-}
-
-int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, const void* R, void* Z, void* Y, const int32_t* offsets, int64_t rows, int experts,
-                               int n_in, int n_out, int act, int join, void* stream)
-{
-    clear_error();
-    if (!X || !W || !Y || !offsets) return fail(TW_INVALID, "NULL tensor pointer");
-    int rc = check_experts(rows, experts, n_in, n_out);
-    if (rc != TW_OK || (rc = check_kind(act, join)) != TW_OK) return rc;
-    if (join == FPDT_TW_JOIN_TIMES && !R) return fail(TW_INVALID, "JOIN_TIMES needs R");
-    for (const void* p : {B, R, (const void*)Z, (const void*)Y})
-        if (misaligned(p, 2)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
-    if (misaligned(X, 16) || misaligned(W, 16)) return fail(TW_INVALID, "X and W must be 16-byte aligned");
-    if (misaligned(offsets, 4)) return fail(TW_INVALID, "offsets is not aligned to its elements");
-    const size_t out = (size_t)rows * n_out * 2;
-    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, (size_t)experts * n_in * n_out * 2, false}, {"B", B, (size_t)experts * n_out * 2, false},
-                        {"R", R, out, false}, {"Z", Z, out, true}, {"Y", Y, out, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
-    const int same[][2] = {{3, 5}};
-    if ((rc = check_apart(args, 7, same, 1)) != TW_OK) return rc;
-    const GroupPlan plan = plan_groups(rows, experts, n_out, n_in);
-    if (plan.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
-    const Groups g = {offsets, experts, (int)rows};
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    by_act(act, [&](auto a) {
-        constexpr int ACT = decltype(a)::value;
-        const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y), join == FPDT_TW_JOIN_TIMES,
-                                      all_wide(n_out, {B, R, Z, Y})};
-        by_tile(plan.wmt, plan.wnt, [&](auto wm, auto wn) {
-            experts_affine_kernel<ACT, decltype(wm)::value, decltype(wn)::value>
-                <<<grid_of(plan.tiles), NTHREAD, 0, st>>>(static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
-        });
-    });
-    HIP_TRY(hipGetLastError());
-    return TW_OK;
-}
-
-int fpdt_tw_experts_linear_bwd(const void* X, const void* W, const void* dY, void* dX, float* dW, const int32_t* offsets, int64_t rows, int experts, int n_in,
-                               int n_out, void* stream)
-{
-    clear_error();
-    if (!X || !W || !dY || !offsets) return fail(TW_INVALID, "NULL tensor pointer");
-    int rc = check_experts(rows, experts, n_in, n_out);
-    if (rc != TW_OK) return rc;
-    if (misaligned(X, 16) || misaligned(W, 16) || misaligned(dY, 16)) return fail(TW_INVALID, "X, W and dY must be 16-byte aligned");
-    if (misaligned(dX, 2) || misaligned(dW, 4) || misaligned(offsets, 4)) return fail(TW_INVALID, "dX, dW or offsets is not aligned to its elements");
-    const size_t weights = (size_t)experts * n_in * n_out;
-    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, weights * 2, false}, {"dY", dY, (size_t)rows * n_out * 2, false},
-                        {"dX", dX, (size_t)rows * n_in * 2, true}, {"dW", dW, weights * 4, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
-    if ((rc = check_apart(args, 6, nullptr, 0)) != TW_OK) return rc;
-    const GroupPlan px = plan_groups(rows, experts, n_in, n_out), pw = plan_weights(rows, experts, n_in, n_out);
-    if (px.tiles > (int64_t)1 << 30 || pw.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
-    const Groups g = {offsets, experts, (int)rows};
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    auto t = [](const void* p) { return static_cast<const uint16_t*>(p); };
-    if (dX)
-        by_tile(px.wmt, px.wnt, [&](auto wm, auto wn) {
-            experts_dx_kernel<decltype(wm)::value, decltype(wn)::value><<<grid_of(px.tiles), NTHREAD, 0, st>>>(t(dY), t(W), static_cast<uint16_t*>(dX), n_in, n_out, g);
-        });
-    if (dW)
-        by_tile(pw.wmt, pw.wnt, [&](auto wm, auto wn) {
-            experts_dw_kernel<decltype(wm)::value, decltype(wn)::value><<<grid_of(pw.tiles), NTHREAD, 0, st>>>(t(X), t(dY), dW, n_in, n_out, g);
-        });
     HIP_TRY(hipGetLastError());
     return TW_OK;
 }

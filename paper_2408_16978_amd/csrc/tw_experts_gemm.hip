@@ -1,0 +1,69 @@
+// The experts' products (include/fpdt_tokenwise.h: fpdt_tw_experts_affine_fwd).
+//
+//     z = x W^T + b,   y = act(z) + r  or  act(z) r          (W, b: of the row's expert)
+#include "tw_experts_gemm.h"
+
+namespace fpdt_tw {
+namespace {
+
+// Rows of X and of what is behind the product begin at the tile's own.
+template <int ACT, int WMT, int WNT>
+__global__ __launch_bounds__(NTHREAD, 1) void experts_affine_kernel(const uint16_t* X, const uint16_t* W, int n_in, int n_out, Groups g, Epilogue<ACT> behind)
+{
+    __shared__ __attribute__((aligned(256))) u32x4 ring[ring_bytes(WMT, WNT) / 16];
+    GroupTile t;
+    if (!find_group(g, 64 * WMT, ((unsigned)n_out + 64 * WNT - 1) / (64 * WNT), t)) return;
+    const int skip = (int)fpdt::uniform((unsigned)t.tile_m) * (64 * WMT), left = t.rows - skip, tile_n = (int)fpdt::uniform((unsigned)t.tile_n);
+    const int64_t first = (int64_t)t.first + skip, out = first * n_out;
+    const Operand a = {X + first * n_in, n_in, left}, b = {W + (int64_t)t.expert * n_out * n_in, n_in, n_out};
+    if (behind.B) behind.B += (int64_t)t.expert * n_out;
+    if (behind.R) behind.R += out;
+    if (behind.Z) behind.Z += out;
+    behind.Y += out;
+    by_rows<WMT>(left, [&](auto w) __attribute__((always_inline)) {
+        product_tile<false, false, false, false, decltype(w)::value, WNT>(ring, a, b, n_in, nullptr, n_out, left, n_out, 0, tile_n, 0, n_in / STAGE_K, false, Whole(), behind);
+    });
+}
+
+}  // namespace
+}  // namespace fpdt_tw
+
+using namespace fpdt_tw;
+
+extern "C" {
+
+int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, const void* R, void* Z, void* Y, const int32_t* offsets, int64_t rows, int experts,
+                               int n_in, int n_out, int act, int join, void* stream)
+{
+    clear_error();
+    if (!X || !W || !Y || !offsets) return fail(TW_INVALID, "NULL tensor pointer");
+    int rc = check_experts(rows, experts, n_in, n_out);
+    if (rc != TW_OK || (rc = check_kind(act, join)) != TW_OK) return rc;
+    if (join == FPDT_TW_JOIN_TIMES && !R) return fail(TW_INVALID, "JOIN_TIMES needs R");
+    for (const void* p : {B, R, (const void*)Z, (const void*)Y})
+        if (misaligned(p, 2)) return fail(TW_INVALID, "a tensor is not aligned to its elements");
+    if (misaligned(X, 16) || misaligned(W, 16)) return fail(TW_INVALID, "X and W must be 16-byte aligned");
+    if (misaligned(offsets, 4)) return fail(TW_INVALID, "offsets is not aligned to its elements");
+    const size_t out = (size_t)rows * n_out * 2;
+    const Arg args[] = {{"X", X, (size_t)rows * n_in * 2, false}, {"W", W, (size_t)experts * n_in * n_out * 2, false}, {"B", B, (size_t)experts * n_out * 2, false},
+                        {"R", R, out, false}, {"Z", Z, out, true}, {"Y", Y, out, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
+    const int same[][2] = {{3, 5}};
+    if ((rc = check_apart(args, 7, same, 1)) != TW_OK) return rc;
+    const GroupPlan plan = plan_groups(rows, experts, n_out, n_in);
+    if (plan.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+    const Groups g = {offsets, experts, (int)rows};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    by_act(act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y), join == FPDT_TW_JOIN_TIMES,
+                                      all_wide(n_out, {B, R, Z, Y})};
+        by_group_tile(plan, [&](auto wm, auto wn) {
+            experts_affine_kernel<ACT, decltype(wm)::value, decltype(wn)::value>
+                <<<grid_of(plan.tiles), NTHREAD, 0, st>>>(static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
+        });
+    });
+    HIP_TRY(hipGetLastError());
+    return TW_OK;
+}
+
+}  // extern "C"

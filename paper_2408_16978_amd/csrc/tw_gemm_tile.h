@@ -210,6 +210,15 @@ __device__ __forceinline__ void tile_of(unsigned id, unsigned tiles_m, unsigned 
     tile_m = (int)(grp * GROUP_M + in_grp % rows_in_grp), tile_n = (int)(in_grp / rows_in_grp);
 }
 
+// The same for an expert's few tile rows, in groups of three to five: a last group of one would share its operand slices with nobody.
+__device__ __forceinline__ void tile_of_few(unsigned id, unsigned tiles_m, unsigned tiles_n, int& tile_m, int& tile_n)
+{
+    const unsigned groups = tiles_m < 6 ? 1 : (tiles_m + 2) / 4, least = tiles_m / groups, more = tiles_m - least * groups;  // the first `more` have one more
+    const unsigned head = more * (least + 1) * tiles_n, in = id < head ? id : id - head, size = id < head ? least + 1 : least;
+    const unsigned grp = in / (size * tiles_n), in_grp = in % (size * tiles_n);
+    tile_m = (int)((id < head ? 0 : more * (least + 1)) + grp * size + in_grp % size), tile_n = (int)(in_grp / size);
+}
+
 // What a workgroup of a product computes: tile (tile_m, tile_n), number `id`, over all of k or (is_part) over its split of it.
 struct Unit {
     unsigned id, split;
@@ -272,8 +281,11 @@ struct Nothing {
 // for the whole loop (with the builtin the allocator moved tiles between the two register files).
 // (B's fragment is the first operand: a lane then holds four consecutive columns of one row of C.)
 #define TW_MFMA(d, x, y) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(y), "v"(x))
+//
+// `ring`: ring_bytes(WMT, WNT) of LDS, 256-byte aligned.
+constexpr unsigned ring_bytes(int wmt, int wnt) { return ((wmt > 1 ? 3 : 2) * wmt + 2 * wnt) * PANEL; }
 template <bool TA, bool TB, bool OUT_F32, bool ACCUM, int WMT, int WNT, class PartOf, class Behind>
-__device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, int K, void* __restrict__ Cout, int64_t ldc, int M, int N, int tile_m,
+__device__ __forceinline__ void product_tile(u32x4* ring, const Operand& A, const Operand& B, int K, void* __restrict__ Cout, int64_t ldc, int M, int N, int tile_m,
                                              int tile_n, int stage0, int unit_stages, bool is_part, PartOf part_of, const Behind& behind)
 {
     // LDS: slots of a stage each, three of A and two of B.  64 x 256 tiles: two of each, so that two workgroups fit a
@@ -283,7 +295,7 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
     constexpr int MI = 2 * WMT, NI = 2 * WNT;                   // accumulator tiles of a wave
     constexpr int NCA = 2 * WMT, NCB = 2 * WNT;                 // copies of a wave per stage
     static_assert(NWAVE == 4, "a wave copies a quarter of every panel");
-    __shared__ __attribute__((aligned(256))) u32x4 ring[LDS_BYTES / 16];
+    static_assert(LDS_BYTES == ring_bytes(WMT, WNT), "");
     const int lane = threadIdx.x & 63;
     const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wu >> 1, wn = wu & 1;
@@ -337,8 +349,8 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
     if (n_full == 0) turn_to_tail();
     first_copies(0);
     if (total > 1) {
-        a_side.pos += a_side.step;
-        b_side.pos += b_side.step;
+        a_side.pos = fpdt::uniform(a_side.pos + a_side.step);
+        b_side.pos = fpdt::uniform(b_side.pos + b_side.step);
         if (n_full == 1) turn_to_tail();
         first_copies(1);
         fpdt::wait_vmem_at_most<NCA + NCB>();
@@ -406,8 +418,8 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
         for (; copied > 0; --copied) {
-            a_side.pos += a_side.step;
-            b_side.pos += b_side.step;
+            a_side.pos = fpdt::uniform(a_side.pos + a_side.step);
+            b_side.pos = fpdt::uniform(b_side.pos + b_side.step);
             half_stage(Ks0{}, std::true_type{}, cur_a, cur_b, copy_lds + free_a, 0u);
             fpdt::wait_vmem_at_most<SPREAD ? NCA : 0>();  // the next stage: all but the copies just issued
             fpdt::barrier_no_fence();  // everyone's part of it; everyone has read all of this one
@@ -416,8 +428,8 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
             next_stage();
         }
         if (pass == 0 && k_left > 0 && n_full >= 2) {
-            a_side.pos += a_side.step;
-            b_side.pos += b_side.step;
+            a_side.pos = fpdt::uniform(a_side.pos + a_side.step);
+            b_side.pos = fpdt::uniform(b_side.pos + b_side.step);
             turn_to_tail();
             copied = 1;
         }

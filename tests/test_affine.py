@@ -90,19 +90,27 @@ def test_workspace_bytes_and_binding():
         TW.fpdt_tw_affine_bwd(x, None, x, x, None, None)
 
 
-def test_compiler_moves_no_accumulator():
-    """As for the other products: between the first MFMA and the wait behind the last one no instruction of the compiler's may touch an accumulation register."""
+@pytest.mark.parametrize("source,count", [("tw_affine.hip", 15), ("tw_experts_gemm.hip", 12), ("tw_experts_gemm_bwd.hip", 8)])
+def test_compiler_moves_no_accumulator(source, count):
+    """As for the other products: from the first MFMA of a tile loop to the wait behind its last one no instruction of the compiler's may touch an accumulation
+    register, and every address that a copy takes from scalar registers is in some."""
     with tempfile.TemporaryDirectory() as d:
-        out = os.path.join(d, "tw_affine.s")
-        subprocess.run([lib_build.HIPCC] + lib_build.FLAGS + ["-S", "--cuda-device-only", os.path.join(lib_build.SRC_DIR, "tw_affine.hip"), "-o", out], check=True, capture_output=True)
+        out = os.path.join(d, "x.s")
+        subprocess.run([lib_build.HIPCC] + lib_build.FLAGS + ["-S", "--cuda-device-only", os.path.join(lib_build.SRC_DIR, source), "-o", out], check=True, capture_output=True)
         with open(out) as f:
             text = f.read()
-    kernels = re.findall(r"^_ZN\S*(?:affine_kernel|experts_d[xw]_kernel)\S*:.*?^\.Lfunc_end", text, re.S | re.M)
-    assert len(kernels) == 40
-    for k in kernels:
-        body = [line.split(";")[0].strip() for line in k.splitlines()]
-        first, last = next(i for i, x in enumerate(body) if "v_mfma" in x), next(i for i, x in enumerate(body) if x == "s_nop 15")
-        assert first < last and not [x for x in body[first:last] if "accvgpr" in x or "scratch" in x], body[0]
+    kernels = [k for k in re.findall(r"^(_ZN\S*):(.*?)^\.Lfunc_end", text, re.S | re.M) if "v_mfma" in k[1]]
+    assert len(kernels) == count
+    for name, k in kernels:
+        loops = False  # from an MFMA on, until the wait
+        for line in (line.split(";")[0].strip() for line in k.splitlines()):
+            if "v_mfma" in line:
+                loops = True
+            elif line == "s_nop 15":
+                loops = False
+            assert not (loops and ("accvgpr" in line or "scratch" in line)), (name, line)
+            assert not re.match(r"s_mov_b64 s\[[0-9:]+\], v", line), (name, line)
+        assert not loops, name
 
 
 # ------------------------------------------------------------------ parity (GPU)
