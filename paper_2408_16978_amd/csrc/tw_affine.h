@@ -28,7 +28,122 @@ template <int ACT> struct Epilogue {
         if (R) y = times ? y * to_float(R[at]) : y + to_float(R[at]);
         Y[at] = from_float<uint16_t>(y);
     }
+    // Four columns of row m from n on (fewer at the end of a row of N), without their bias yet.
+    __device__ __forceinline__ void four(floatx4 v, int m, int n, int N) const
+    {
+        const int64_t c = (int64_t)m * N + n;
+        if (wide) {  // (N is a multiple of 8)
+            if (B) {
+                const auto b = load<4>(B + n);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] += to_float(b.e[r]);
+            }
+            float y[4];
+            if (Z) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = v[r];
+                store(Z + c, rounded<4>(y, uint16_t()));
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = act(v[r]);
+            if (R) {
+                const auto j = load<4>(R + c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = times ? y[r] * to_float(j.e[r]) : y[r] + to_float(j.e[r]);
+            }
+            store(Y + c, rounded<4>(y, uint16_t()));
+        } else {
+            for (int r = 0; r < 4 && n + r < N; ++r) one(v[r] + (B ? to_float(B[n + r]) : 0.f), c + r);
+        }
+    }
 };
+
+// ---- few rows -------------------------------------------------------------------------------
+// The product of M <= 16 MT rows with 16 columns (rows of W) from n0 on, and what is behind it, by one workgroup of FEW_WAVES waves: a wave takes every
+// FEW_WAVES-th 64 of k, fragments straight from memory (no other workgroup reads these rows of W; those of X come from L2), and the
+// waves' sums are added in LDS.  Bound by the memory, that is by the bytes under way: the fragments of the next U units are requested before
+// the MFMAs of these, and there is no barrier but the last.  16 rows, weights that come from HBM, us: 4096 x 4096 11.4 (tiles of 64 x 256 in 16 splits and
+// their sums 19.7), 1024 x 1024 4.3 (9.1), 2560 x 10240 20.4 (21.0), but 4096 x 14336 35.3 (29.8).  32 columns a workgroup, which read X half as often, took
+// 15.5, 5.1, 21.7 and 30.9; loads of W past the caches, which fetch a line for each half of it, 11.6, 4.5, 22.7 and 36.9.
+constexpr int FEW_WAVES = 8, FEW_ROWS = 64, FEW_COLS = 16;
+template <int ACT, int MT> __device__ __forceinline__ void few_rows(float* sums, const uint16_t* X, const uint16_t* W, int K, int M, int N, int n0, const Epilogue<ACT>& behind)
+{
+    constexpr int U = 2;  // units of 64 k
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fk = 8 * (lane >> 4);
+    // rows behind the operands are read as the last one: their products are not stored
+    const uint16_t *w = W + (int64_t)(n0 + fr < N ? n0 + fr : N - 1) * K + fk + 64 * wave, *x[MT];
+    floatx4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        x[i] = X + (int64_t)(16 * i + fr < M ? 16 * i + fr : M - 1) * K + fk + 64 * wave;
+        acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Some {
+        bf16x8 a[U][2], b[U][2][MT];
+    };
+    constexpr int STEP = 64 * FEW_WAVES;  // from a wave's unit to its next one
+    auto fetch = [&](Some& s, int k0, auto whole_tag) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole_tag)::value;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + STEP * u + 32 * h;
+                const bool in = WHOLE || 64 * wave + k + fk < K;  // (K is a multiple of 8)
+                s.a[u][h] = in ? *reinterpret_cast<const bf16x8*>(w + k) : bf16x8{};
+#pragma unroll
+                for (int i = 0; i < MT; ++i) s.b[u][h][i] = in ? *reinterpret_cast<const bf16x8*>(x[i] + k) : bf16x8{};
+            }
+    };
+    auto add = [&](const Some& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s.a[u][h], s.b[u][h][i], acc[i], 0, 0, 0);
+    };
+    const int mine = (K / 64 - wave + FEW_WAVES - 1) / FEW_WAVES, whole = mine > 0 ? mine / U : 0;  // this wave's whole units, and pairs of them
+    Some s0, s1;
+    if (whole > 0) {
+        fetch(s0, 0, std::true_type{});
+        int i = 0;
+        for (; i + 2 < whole; i += 2) {  // (nothing is conditional in here: a wait counts what is under way)
+            fetch(s1, STEP * U * (i + 1), std::true_type{});
+            __builtin_amdgcn_sched_barrier(0);
+            add(s0);
+            fetch(s0, STEP * U * (i + 2), std::true_type{});
+            __builtin_amdgcn_sched_barrier(0);
+            add(s1);
+        }
+        if (i + 1 < whole) {
+            fetch(s1, STEP * U * (i + 1), std::true_type{});
+            add(s0);
+            add(s1);
+        } else {
+            add(s0);
+        }
+    }
+    if (64 * wave + STEP * U * whole < K) {
+        fetch(s0, STEP * U * whole, std::false_type{});
+        add(s0);
+    }
+    // a lane has columns 4 (lane / 16) .. + 3 of row lane % 16
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<floatx4*>(sums + ((wave * MT + i) * 64 + lane) * 4) = acc[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < MT * 64; t += FEW_WAVES * 64) {
+        floatx4 v = *reinterpret_cast<const floatx4*>(sums + t * 4);
+#pragma unroll
+        for (int s = 1; s < FEW_WAVES; ++s) v += *reinterpret_cast<const floatx4*>(sums + (s * MT * 64 + t) * 4);
+        const int m = 16 * (t / 64) + t % 16, n = n0 + 4 * (t % 64 / 16);
+        if (m < M && n < N) behind.four(v, m, n, N);
+    }
+}
+// Every 16 columns read X anew: it pays while that is not much.  Measured, us, few_rows and tiles: 1 row, 4096 x 14336 24.8 and 31.2; 32 rows, 4096 x 4096 15.0 and 19.1,
+// 14336 x 4096 44.7 and 33.1; 64 rows, 1024 x 1024 7.0 and 9.2, 4096 x 4096 22.7 and 19.3; 16 rows, 14336 x 4096 31.7 and 33.8, 4096 x 14336 35.3 and 29.8.
+inline bool few_pays(int64_t rows, int64_t weights) { return rows * weights <= (int64_t)16 * 34 << 20; }
+template <int MT> constexpr int few_lds = FEW_WAVES * MT * 64 * 4;  // floats
 
 // Where expert e's rows begin and end, whatever the offsets say within the rows that there are.
 __device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int rows)

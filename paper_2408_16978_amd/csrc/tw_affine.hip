@@ -41,30 +41,13 @@ __global__ __launch_bounds__(256) void affine_sum_kernel(const float* part, Unit
     const float* p = part + (size_t)i * tm * tn + at;
     floatx4 v = *reinterpret_cast<const floatx4*>(p);
     for (int s = 1; s < u.splits; ++s) v += *reinterpret_cast<const floatx4*>(p + s * stride);
-    const int64_t c = (int64_t)m * N + n;
-    if (behind.wide) {  // (N is a multiple of 8)
-        if (behind.B) {
-            const auto b = load<4>(behind.B + n);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] += to_float(b.e[r]);
-        }
-        float y[4];
-        if (behind.Z) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = v[r];
-            store(behind.Z + c, rounded<4>(y, uint16_t()));
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = behind.act(v[r]);
-        if (behind.R) {
-            const auto j = load<4>(behind.R + c);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = behind.times ? y[r] * to_float(j.e[r]) : y[r] + to_float(j.e[r]);
-        }
-        store(behind.Y + c, rounded<4>(y, uint16_t()));
-    } else {
-        for (int r = 0; r < 4 && n + r < N; ++r) behind.one(v[r] + (behind.B ? to_float(behind.B[n + r]) : 0.f), c + r);
-    }
+    behind.four(v, m, n, N);
+}
+
+template <int ACT, int MT> __global__ __launch_bounds__(FEW_WAVES * 64) void affine_few_kernel(const uint16_t* X, const uint16_t* W, int K, int M, int N, Epilogue<ACT> behind)
+{
+    __shared__ __attribute__((aligned(16))) float sums[few_lds<MT>];
+    few_rows<ACT, MT>(sums, X, W, K, M, N, blockIdx.x * FEW_COLS, behind);
 }
 
 // ---- backward of what is behind a product -------------------------------------------------
@@ -90,7 +73,7 @@ __device__ __forceinline__ int64_t start_of(const int32_t* offsets, int e, int64
 
 template <int ACT, bool TIMES, bool WHOLE> __global__ __launch_bounds__(256) void affine_bwd_kernel(Backward b)
 {
-    constexpr int V = 8, U = 2;
+    constexpr int V = 8, U = 4;
     constexpr bool BEHIND = TIMES || ACT != FPDT_TW_ACT_NONE;
     __shared__ float lds[256 * V];
     const int tc = threadIdx.x % b.cols, tr = threadIdx.x / b.cols, lines = 256 / b.cols, c = ((int)blockIdx.x * b.cols + tc) * V, left = b.n - c;
@@ -124,40 +107,40 @@ template <int ACT, bool TIMES, bool WHOLE> __global__ __launch_bounds__(256) voi
         int64_t end = start_of(b.offsets, e + 1, b.rows);
         end = end > row && end < last ? end : last;
         float sum[V] = {};
-        if (left > 0)
-            for (int64_t r0 = row + tr; r0 < end; r0 += U * lines) {
-                Vec<uint16_t, V> dy[U], z[U], r[U];
+        // n rows from r on, `lines` apart: all of them are requested first, and nothing is conditional, so that no wait for them is one for the rows stored before
+        auto rows = [&](int64_t r, auto n_tag) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_tag)::value;
+            const int64_t at0 = r * b.n + c, step = (int64_t)lines * b.n;
+            Vec<uint16_t, V> dy[n], z[n], gate[n];
 #pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    const int64_t at = (r0 + k * lines) * b.n + c;
-                    if (r0 + k * lines >= end) break;
-                    dy[k] = fetch(b.dY, at);
-                    if (BEHIND && ACT != FPDT_TW_ACT_NONE) z[k] = fetch(b.Z, at);
-                    if (TIMES && ACT == FPDT_TW_ACT_NONE) z[k] = fetch(b.Z, at);
-                    if (TIMES) r[k] = fetch(b.R, at);
-                }
-#pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    const int64_t at = (r0 + k * lines) * b.n + c;
-                    if (r0 + k * lines >= end) break;
-                    float dz[V], dr[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float g = to_float(dy[k].e[i]);
-                        if (BEHIND) {
-                            float y;
-                            const float slope = slope_of<ACT>(to_float(z[k].e[i]), y);
-                            dz[i] = g * slope;
-                            if (TIMES) dz[i] *= to_float(r[k].e[i]), dr[i] = g * y;
-                        } else {
-                            dz[i] = g;
-                        }
-                        sum[i] += dz[i];
-                    }
-                    if (b.dZ) put(b.dZ, at, rounded<V>(dz, uint16_t()));
-                    if (TIMES && b.dR) put(b.dR, at, rounded<V>(dr, uint16_t()));
-                }
+            for (int k = 0; k < n; ++k) {
+                dy[k] = fetch(b.dY, at0 + k * step);
+                if (BEHIND) z[k] = fetch(b.Z, at0 + k * step);
+                if (TIMES) gate[k] = fetch(b.R, at0 + k * step);
             }
+#pragma unroll
+            for (int k = 0; k < n; ++k) {
+                float dz[V], dr[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float g = to_float(dy[k].e[i]);
+                    dz[i] = g;
+                    if (BEHIND) {
+                        float y;
+                        dz[i] *= slope_of<ACT>(to_float(z[k].e[i]), y);
+                        if (TIMES) dz[i] *= to_float(gate[k].e[i]), dr[i] = g * y;
+                    }
+                    sum[i] += dz[i];
+                }
+                if (BEHIND || b.dZ) put(b.dZ, at0 + k * step, rounded<V>(dz, uint16_t()));
+                if (TIMES && b.dR) put(b.dR, at0 + k * step, rounded<V>(dr, uint16_t()));
+            }
+        };
+        if (left > 0) {
+            int64_t r = row + tr;
+            for (; r + (U - 1) * lines < end; r += U * lines) rows(r, Int<U>());
+            for (; r < end; r += lines) rows(r, Int<1>());
+        }
         if (b.partial) {
             float* out = b.partial + ((int64_t)blockIdx.y + e) * b.n;
 #pragma unroll
@@ -233,18 +216,28 @@ Layout layout_of(int64_t rows, int n_in, int n_out)
     return l;
 }
 
+// Threads along the columns: the most of which at most a ninth are idle, or those of which the fewest are (30001 rows of 2560 columns, SILU: 256 threads, a quarter
+// of the second 256 at work, 104 us, 64 87; 100000 rows of 264 columns: 8 threads 76 us, 64 56).
 int lanes_of(int n)
 {
-    int cols = 8;
-    while (cols < 256 && cols * 8 < n) cols *= 2;
-    return cols;
+    const int accesses = (n + 7) / 8;
+    int best = 8, least = 1 << 30;
+    while (best < 32 && best < accesses) best *= 2;
+    if (accesses < 32) return best;
+    for (int cols = 256; cols >= 32; cols /= 2) {
+        const int threads = (accesses + cols - 1) / cols * cols;
+        if (threads * 8 <= accesses * 9) return cols;
+        if (threads < least) best = cols, least = threads;
+    }
+    return best;
 }
-// Rows of a slice: 2048 workgroups where there are rows enough, so that partial sums stay a small part of the tensors, and two rows a thread at least.
+// Rows of a slice: 1536 workgroups where there are rows enough, so that partial sums stay a small part of the tensors, and two rows a thread at
+// least (16384 rows of 10240 columns, GELU, us: 1024 workgroups 212, 1536 200, 2048 204).
 int64_t slice_of(int64_t rows, int n)
 {
-    const int cols = lanes_of(n), wide = (n + cols * 8 - 1) / (cols * 8);
-    const int64_t most = wide < 2048 ? 2048 / wide : 1, slice = (rows + most - 1) / most, least = 2 * (256 / cols);
-    return slice > least ? slice : least;
+    const int cols = lanes_of(n), wide = (n + cols * 8 - 1) / (cols * 8), lines = 256 / cols;
+    const int64_t most = wide < 1536 ? 1536 / wide : 1, least = 2 * lines, slice = (rows + most - 1) / most;
+    return slice > least ? (slice + lines - 1) / lines * lines : least;
 }
 
 }  // namespace
@@ -291,6 +284,18 @@ int fpdt_tw_affine_fwd(const void* X, const void* W, const void* B, const void* 
         realign(W, n_out, n_in, n_in, ws, w.ld, st);
     }
     const bool wide = all_wide(n_out, {B, R, Z, Y});
+    const int tall = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (rows <= FEW_ROWS && n_in % 8 == 0 && few_pays(rows, (int64_t)n_in * n_out)) {
+        by_act(act, [&](auto a) {
+            constexpr int ACT = decltype(a)::value;
+            const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y),
+                                          join == FPDT_TW_JOIN_TIMES, wide};
+            const auto kernel = tall == 1 ? affine_few_kernel<ACT, 1> : tall == 2 ? affine_few_kernel<ACT, 2> : affine_few_kernel<ACT, 4>;
+            kernel<<<(unsigned)((n_out + FEW_COLS - 1) / FEW_COLS), FEW_WAVES * 64, 0, st>>>(static_cast<const uint16_t*>(X), w.p, n_in, (int)rows, n_out, behind);
+        });
+        HIP_TRY(hipGetLastError());
+        return TW_OK;
+    }
     for (int64_t r0 = 0; r0 < rows; r0 += l.piece) {
         const int m = (int)(rows - r0 < l.piece ? rows - r0 : l.piece);
         const Plan plan = plan_of(m, n_in, n_out);

@@ -127,8 +127,11 @@ __global__ __launch_bounds__(THREADS) void sort_place_kernel(Sort s)
 }
 
 // ---- rows -----------------------------------------------------------------------------------
-// A wave takes CHUNK neighbouring accesses of 16 bytes a lane of one row at a time; the last access of a row may be cut off (WHOLE: none is).
-constexpr int SMALL = 256, CHUNK = 4;
+// A wave takes CHUNK accesses of 16 bytes a lane of one row at a time: 1024 elements (bf16, us, 512 | 1024 | 2048 | 4096: sums over two places of 32768 tokens of
+// 4096 141 | 128 | 138 | 151, the gradient of 60000 tokens of 1024 in four places 173 | 174 | 234 | 425; fp32, gradient of 20000 of 4096 in two,
+// 316 with 256, 307 with 512, 297 with 1024).  The last access of a row may be cut off (WHOLE: none is).
+constexpr int SMALL = 256;
+template <class T> constexpr int chunk_of = sizeof(T);
 template <bool WHOLE, int V, class T> __device__ __forceinline__ Vec<T, V> take(const T* p, int c, int hidden, bool once)
 {
     if (WHOLE || c + V <= hidden) return once ? load_once<V>(p + c) : load<V>(p + c);
@@ -161,10 +164,10 @@ __device__ __forceinline__ int64_t place_of(const Rows& s, int64_t a)
 }
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
 
-// xs[place(t, j)] = x[t]
+// xs[place(t, j)] = x[t].  (Read through the caches: 32768 tokens of 4096 to two places 125 us, past them 148.)
 template <class T, bool WHOLE> __global__ __launch_bounds__(SMALL) void gather_kernel(const T* X, T* Xs, Rows s, int chunks)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), CHUNK = chunk_of<T>;
     const int lane = threadIdx.x & 63;
     for (int64_t unit = (int64_t)blockIdx.x * (SMALL / 64) + wave_id(); unit < s.rows * chunks; unit += (int64_t)gridDim.x * (SMALL / 64)) {
         const int64_t t = unit / chunks;
@@ -172,7 +175,7 @@ template <class T, bool WHOLE> __global__ __launch_bounds__(SMALL) void gather_k
         Vec<T, V> x[CHUNK];
 #pragma unroll
         for (int k = 0; k < CHUNK; ++k)
-            if (c0 + k * 64 * V < s.hidden) x[k] = take<WHOLE, V>(X + t * s.hidden, c0 + k * 64 * V, s.hidden, true);
+            if (c0 + k * 64 * V < s.hidden) x[k] = take<WHOLE, V>(X + t * s.hidden, c0 + k * 64 * V, s.hidden, false);
         for (int j = 0; j < s.top; ++j) {
             const int64_t p = place_of(s, t * s.top + j);
             if (p < 0) continue;
@@ -186,7 +189,7 @@ template <class T, bool WHOLE> __global__ __launch_bounds__(SMALL) void gather_k
 // y[t] = sum_j (w(t, j)) ys[place(t, j)] (+ r[t])
 template <class T, bool WEIGHTED, bool WHOLE> __global__ __launch_bounds__(SMALL) void combine_kernel(const T* Ys, const T* R, T* Y, Rows s, int chunks)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), CHUNK = chunk_of<T>;
     const int lane = threadIdx.x & 63;
     for (int64_t unit = (int64_t)blockIdx.x * (SMALL / 64) + wave_id(); unit < s.rows * chunks; unit += (int64_t)gridDim.x * (SMALL / 64)) {
         const int64_t t = unit / chunks;
@@ -225,7 +228,7 @@ template <class T, bool WEIGHTED, bool WHOLE> __global__ __launch_bounds__(SMALL
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(SMALL) void combine_bwd_kernel(const T* Ys, const T* dY, T* dYs, float* dweight, Rows s, int tokens)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), CHUNK = chunk_of<T>;
     const int lane = threadIdx.x & 63;
     const int64_t first = (int64_t)blockIdx.x * tokens * s.top, end = first + (int64_t)tokens * s.top, last = end < s.rows * s.top ? end : s.rows * s.top;
     for (int64_t a = first + wave_id(); a < last; a += SMALL / 64) {
@@ -315,7 +318,7 @@ template <class F> void by_type(int dtype, int hidden, F f)
         else f(uint16_t(), std::false_type());
     }
 }
-int chunks_of(int hidden, int size) { return (int)(((int64_t)hidden * size + CHUNK * 1024 - 1) / (CHUNK * 1024)); }
+int chunks_of(int hidden) { return (hidden + 1023) / 1024; }  // (1024 elements in either type)
 unsigned unit_grid(int64_t units)
 {
     const int64_t n = (units + SMALL / 64 - 1) / (SMALL / 64);
@@ -336,7 +339,7 @@ int gathered_sum(const void* In, const float* weight, const int32_t* place, cons
     const Arg in[] = {{In, one * top}, {weight, index}, {place, index}, {R, one}};
     if (meets({Out, one}, in, 4, R)) return fail(TW_INVALID, "the output overlaps another tensor");
     const Rows s = {place, weight, rows, rows * top, top, hidden};
-    const int chunks = chunks_of(hidden, (int)size);
+    const int chunks = chunks_of(hidden);
     by_type(dtype, hidden, [&](auto type, auto whole) {
         typedef decltype(type) T;
         constexpr bool WHOLE = decltype(whole)::value;
@@ -395,7 +398,7 @@ int fpdt_tw_experts_gather_fwd(const void* X, const int32_t* place, void* Xs, in
     const Arg in[] = {{X, one}, {place, (size_t)rows * top * 4}};
     if (meets({Xs, one * top}, in, 2)) return fail(TW_INVALID, "Xs overlaps another tensor");
     const Rows s = {place, nullptr, rows, rows * top, top, hidden};
-    const int chunks = chunks_of(hidden, (int)size);
+    const int chunks = chunks_of(hidden);
     hipStream_t st = static_cast<hipStream_t>(stream);
     by_type(dtype, hidden, [&](auto type, auto whole) {
         typedef decltype(type) T;

@@ -25,6 +25,24 @@ __global__ __launch_bounds__(NTHREAD, 1) void experts_affine_kernel(const uint16
     });
 }
 
+// Few rows in all, and so of each expert (blockIdx.y): 16 at a time.
+template <int ACT> __global__ __launch_bounds__(FEW_WAVES * 64) void experts_few_kernel(const uint16_t* X, const uint16_t* W, int n_in, int n_out, Groups g, Epilogue<ACT> behind)
+{
+    __shared__ __attribute__((aligned(16))) float sums[few_lds<1>];
+    const int e = blockIdx.y, first = offset_of(g.offsets, e, g.rows), rows = offset_of(g.offsets, e + 1, g.rows) - first;
+    if (rows <= 0) return;
+    if (behind.B) behind.B += (int64_t)e * n_out;
+    for (int m = 0; m < rows; m += 16) {
+        const int64_t out = (int64_t)(first + m) * n_out;
+        Epilogue<ACT> here = behind;
+        if (here.R) here.R += out;
+        if (here.Z) here.Z += out;
+        here.Y += out;
+        if (m) __syncthreads();  // the sums of the rows before have been read
+        few_rows<ACT, 1>(sums, X + (int64_t)(first + m) * n_in, W + (int64_t)e * n_out * n_in, n_in, rows - m < 16 ? rows - m : 16, n_out, blockIdx.x * FEW_COLS, here);
+    }
+}
+
 }  // namespace
 }  // namespace fpdt_tw
 
@@ -57,6 +75,13 @@ int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, cons
         constexpr int ACT = decltype(a)::value;
         const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y), join == FPDT_TW_JOIN_TIMES,
                                       all_wide(n_out, {B, R, Z, Y})};
+        // (rows that are few for each expert, or weights that are: us, 8 experts of 4096 x 14336, 8 rows 90, tiles 108, 32 rows 173 and 188, 64 rows 203 and
+        // 196; 64 of 2048 x 1536, 64 rows 57 and 76; 4 of 1024 x 1024, 64 rows 6.9 and 12.0)
+        if (rows <= FEW_ROWS && (rows <= 4 * experts || few_pays(16, (int64_t)experts * n_in * n_out))) {
+            experts_few_kernel<ACT><<<dim3((unsigned)((n_out + FEW_COLS - 1) / FEW_COLS), (unsigned)experts), FEW_WAVES * 64, 0, st>>>(
+                static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
+            return;
+        }
         by_group_tile(plan, [&](auto wm, auto wn) {
             experts_affine_kernel<ACT, decltype(wm)::value, decltype(wn)::value>
                 <<<grid_of(plan.tiles), NTHREAD, 0, st>>>(static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
