@@ -217,7 +217,7 @@ Layout layout_of(int64_t rows, int n_in, int n_out)
 }
 
 // Threads along the columns: the most of which at most a ninth are idle, or those of which the fewest are (30001 rows of 2560 columns, SILU: 256 threads, a quarter
-// of the second 256 at work, 104 us, 64 87; 100000 rows of 264 columns: 8 threads 76 us, 64 56).
+// of the second 256 at work, 104 us, 64 87; 100000 rows of 264 columns: 8 threads 76 us, 64 40).
 int lanes_of(int n)
 {
     const int accesses = (n + 7) / 8;

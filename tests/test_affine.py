@@ -171,6 +171,33 @@ def test_gpu_forward(rows, n_in, n_out, act):
         assert torch.equal(Y2, Y)
 
 
+def reference(X, W, B, R, act, times):
+    """The forward in 64 bits on the GPU, with what budget_fwd allows (sizes that numpy's erf would take long for)."""
+    z = X.double() @ W.double().t() + (0.0 if B is None else B.double())
+    y = {"none": lambda v: v, "gelu": lambda v: v * torch.special.erfc(-v / 2 ** 0.5) / 2, "silu": lambda v: v * torch.sigmoid(v)}[act](z)
+    dz = (X.shape[1] + 2) * 2.0 ** -24 * (X.double().abs() @ W.double().abs().t() + (0.0 if B is None else B.double().abs()))
+    dy = 1.13 * dz + (2.0 ** -20 + 2.0 ** -23 * (1 + z * z)) * y.abs()
+    r = None if R is None else R.double()
+    if r is not None:
+        y, dy = (y * r, dy * r.abs()) if times else (y + r, dy + 2.0 ** -22 * (y.abs() + r.abs()))
+    return y, dy + (HALF + 2.0 ** -22) * y.abs(), z, dz + HALF * z.abs()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,n_out", [(4096, 4096), (2500, 4104), (1500, 6144), (600, 1024), (16001, 1280)])
+@pytest.mark.parametrize("n_in", [8, 40, 64, 72, 128, 136, 192, 200, 264, 448, 1000])
+def test_gpu_forward_of_large_tiles(rows, n_out, n_in):
+    """Tiles of every height, whole and cut off, over one, two and three stages of k, whole and cut off: what joins a tile is requested in front of the last two."""
+    X, W, B, R, _ = _make(rows, n_in, n_out, n_in)
+    ws = torch.empty(TW.fpdt_tw_affine_workspace_bytes(rows, n_in, n_out), dtype=torch.uint8, device="cuda")
+    print("[case] large tiles", rows, n_in, n_out, flush=True)
+    for b, r, act, times in ((B, R, "silu", True), (None, R, "none", False), (B, None, "gelu", False)):
+        Y, Z = (torch.full((rows, n_out), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        TW.fpdt_tw_affine_fwd(X, W, b, r, Z, Y, ACT[act], TW.FPDT_TW_JOIN_TIMES if times else TW.FPDT_TW_JOIN_ADD, ws)
+        y, ty, z, tz = reference(X, W, b, r, act, times)
+        assert bool(((Y.double() - y).abs() <= ty).all()) and bool(((Z.double() - z).abs() <= tz).all()), (act, times)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n_in,n_out", [(64, 48), (63, 47)])
 def test_gpu_forward_off_alignment_and_no_further(n_in, n_out):

@@ -281,6 +281,56 @@ def test_gpu_products_of_experts(counts, n_in, n_out, act, join):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("counts,n_in,n_out", [((700, 130, 70, 0, 300, 257), 136, 8192), ((1000, 1, 513, 2000), 64, 4096), ((600,) * 6 + (190, 60), 200, 4104), ((3000, 2000), 520, 2048)])
+def test_gpu_products_of_experts_in_large_tiles(counts, n_in, n_out):
+    """Tiles of 256 rows and what an expert's last rows make of them, with a gate and without; forward and backward against 64 bits on the GPU."""
+    import test_affine
+    E, rows, ends = len(counts), sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    offsets = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(n_in)
+    bf = lambda *s, std=1.0: (torch.randn(*s, device="cuda", generator=g) * std).to(torch.bfloat16)
+    X, W, B, R, dY = bf(rows, n_in), bf(E, n_out, n_in, std=n_in ** -0.5), bf(E, n_out), bf(rows, n_out), bf(rows, n_out, std=0.1)
+    print("[case] large tiles of experts", counts, n_in, n_out, flush=True)
+    dX, dW = torch.full_like(X, 9.0), torch.zeros(E, n_out, n_in, device="cuda")
+    TW.fpdt_tw_experts_linear_bwd(X, W, dY, dX, dW, offsets)
+    for r, act, code in ((R, "silu", TW.FPDT_TW_JOIN_TIMES), (None, "gelu", TW.FPDT_TW_JOIN_ADD)):
+        Y, Z = (torch.full((rows, n_out), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        TW.fpdt_tw_experts_affine_fwd(X, W, B, r, Z, Y, offsets, ACT[act], code)
+        for e in range(E):
+            at = slice(int(ends[e]), int(ends[e + 1]))
+            y, ty, z, tz = test_affine.reference(X[at], W[e], B[e], None if r is None else r[at], act, r is not None)
+            assert bool(((Y[at].double() - y).abs() <= ty).all()) and bool(((Z[at].double() - z).abs() <= tz).all()), (e, act)
+    for e in range(E):
+        at = slice(int(ends[e]), int(ends[e + 1]))
+        x, d, w = X[at].double(), dY[at].double(), W[e].double()
+        want = d @ w
+        assert bool(((dX[at].double() - want).abs() <= (n_out + 2) * 2.0 ** -24 * (d.abs() @ w.abs()) + 2.0 ** -8 * want.abs()).all()), e
+        assert bool(((dW[e].double() - d.t() @ x).abs() <= (counts[e] + 2) * 2.0 ** -24 * (d.abs().t() @ x.abs())).all()), e
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [(0, 3, 17, 0, 40, 4), (64,), (0, 64, 0, 0), (1,) * 60, (16, 16, 16, 16)])
+@pytest.mark.parametrize("n_in,n_out", [(8, 24), (72, 40), (520, 136), (2056, 1000), (4096, 512)])
+def test_gpu_few_rows_of_experts(counts, n_in, n_out):
+    """Up to 64 rows in all, and up to 64 of one expert: 16 at a time, the last ones fewer."""
+    import test_affine
+    E, used, ends = len(counts), sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    rows = min(64, used + 2)
+    offsets = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(n_in)
+    bf = lambda *s, std=1.0: (torch.randn(*s, device="cuda", generator=g) * std).to(torch.bfloat16)
+    X, W, B, R = bf(rows, n_in), bf(E, n_out, n_in, std=n_in ** -0.5), bf(E, n_out), bf(rows, n_out)
+    for r, act, code in ((R, "silu", TW.FPDT_TW_JOIN_TIMES), (None, "gelu", TW.FPDT_TW_JOIN_ADD)):
+        Y, Z = (torch.full((rows, n_out), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        TW.fpdt_tw_experts_affine_fwd(X, W, B, r, Z, Y, offsets, ACT[act], code)
+        for e in range(E):
+            at = slice(int(ends[e]), int(ends[e + 1]))
+            y, ty, z, tz = test_affine.reference(X[at], W[e], B[e], None if r is None else r[at], act, r is not None)
+            assert bool(((Y[at].double() - y).abs() <= ty).all()) and bool(((Z[at].double() - z).abs() <= tz).all()), (e, act)
+        assert (Y[used:] == 9).all() and (Z[used:] == 9).all()
+
+
+@pytest.mark.gpu
 def test_gpu_offsets_that_are_none():
     """Offsets below 0, beyond the rows or descending: no row outside the tensors is read or written, and what is in order is right."""
     E, rows, n = 4, 100, 64
