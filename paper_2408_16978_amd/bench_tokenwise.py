@@ -1,7 +1,8 @@
 """Throughput and workspace of the token-wise chunked operations (include/fpdt_tokenwise.h) as a
 function of the chunk count, at Llama-8B layer shapes, and of the operations around them that are
 not chunked (rotary positions with the QKV split, normalisation, gradient norm, AdamW) in bytes a
-second.  Prints one JSON line per (operation, chunk count).  `python -m paper_2408_16978_amd.bench_tokenwise [--rows 65536] [--chunks 1,4,16,64]`.
+second; with --feed-forward also of products with something behind them, dropout, tokens to experts
+and back and the experts' products.  Prints one JSON line per (operation, chunk count).  `python -m paper_2408_16978_amd.bench_tokenwise [--rows 65536] [--chunks 1,4,16,64]`.
 """
 import argparse
 import json
@@ -33,6 +34,7 @@ def main():
     ap.add_argument("--vocab", type=int, default=128256)
     ap.add_argument("--chunks", default="1,2,4,8,16,64")
     ap.add_argument("--iters", type=int, default=3)
+    ap.add_argument("--feed-forward", action="store_true", help="time the parts of a feed-forward block, dense and with experts, too")
     ap.add_argument("--max-workspace-gib", type=float, default=64.0)
     a = ap.parse_args()
     if not torch.cuda.is_available():
@@ -78,6 +80,8 @@ def main():
             print(json.dumps(rec), flush=True)
     del dW1, dW3, dW2, dWq, dWv, W1, W3, W2, Wq, Wv, X, dY, Y, dX, Yq, loss, lse
     unchunked(rows, nm, nf, nq, a.head_dim, a.iters, bf)
+    if a.feed_forward:
+        feed_forward(rows, nm, nf, a.iters, bf)
 
 
 def split_of(nm, nq, D):
@@ -121,6 +125,46 @@ def unchunked(rows, nm, nf, nq, D, iters, bf):
     for name, nbytes, fn in ops:
         ms = _time(fn, max(iters, 10))
         print(json.dumps({"op": name, "rows": rows, "n_chunks": None, "ms": round(ms, 4), "tbytes_per_s": round(nbytes / ms * 1e-9, 2)}), flush=True)
+
+
+def feed_forward(rows, nm, nf, iters, bf, E=8, top=2):
+    """The feed-forward block's first product with bias and GELU, with a gate, and their gradient; dropout with the residual; `rows` tokens' assignments to `top` of E
+    experts (rows / top tokens) and the experts' products, of weights half as wide.  Widths that experts do not take are left out."""
+    dev, e32 = "cuda", lambda *s: torch.zeros(*s, device="cuda")
+    X, W, B = bf(rows, nm), bf(nf, nm, std=nm ** -0.5), bf(nf)
+    Y, Z, R = (torch.empty(rows, nf, dtype=torch.bfloat16, device=dev) for _ in range(3))
+    R.normal_()
+    dB, S = e32(nf), bf(rows, nm)
+    out = torch.empty_like(X)
+    ws = torch.empty(TW.fpdt_tw_affine_workspace_bytes(rows, nm, nf), dtype=torch.uint8, device=dev)
+    wb = torch.empty(TW.fpdt_tw_affine_bwd_workspace_bytes(rows, nf), dtype=torch.uint8, device=dev)
+    product, wide = 2.0 * rows * nm * nf, 2 * rows * nf
+    gelu, silu, times = TW.FPDT_TW_ACT_GELU, TW.FPDT_TW_ACT_SILU, TW.FPDT_TW_JOIN_TIMES
+    ops = [("affine_gelu_fwd", "tflops", product, lambda: TW.fpdt_tw_affine_fwd(X, W, B, None, Z, Y, gelu, workspace=ws)),
+           ("affine_gate_fwd", "tflops", product, lambda: TW.fpdt_tw_affine_fwd(X, W, None, R, Z, Y, silu, times, ws)),
+           ("affine_gelu_bwd", "tbytes_per_s", 3 * wide, lambda: TW.fpdt_tw_affine_bwd(Z, None, Y, Y, None, dB, gelu, workspace=wb)),
+           ("dropout_residual_fwd", "tbytes_per_s", 6 * rows * nm, lambda: TW.fpdt_tw_dropout_fwd(X, S, out, 0.1, 1))]
+    tokens, half = rows // top, nf // 2
+    if tokens and nm % 8 == 0 and half % 8 == 0 and half:
+        sent = tokens * top
+        expert = torch.rand(tokens, E, device=dev).topk(top, 1).indices.to(torch.int32).contiguous()
+        offsets, place, weight = (torch.zeros(E + 1, dtype=torch.int32, device=dev), torch.zeros_like(expert), torch.rand(tokens, top, device=dev))
+        wsort = torch.empty(TW.fpdt_tw_experts_sort_workspace_bytes(sent, E), dtype=torch.uint8, device=dev)
+        We, dWe, Xs, H, dys, dweight = bf(E, half, nm, std=nm ** -0.5), e32(E, half, nm), bf(sent, nm), bf(sent, half), bf(sent, nm), e32(tokens, top)
+        one, many = 2 * tokens * nm, 2 * sent * nm
+
+        def dispatch():
+            TW.fpdt_tw_experts_sort(expert, offsets, place, wsort)
+            TW.fpdt_tw_experts_gather_fwd(X[:tokens], place, Xs)
+
+        ops += [("experts_sort_gather", "tbytes_per_s", one + many, dispatch),
+                ("experts_combine_fwd", "tbytes_per_s", one + many, lambda: TW.fpdt_tw_experts_combine_fwd(Xs, weight, place, None, out[:tokens])),
+                ("experts_combine_bwd", "tbytes_per_s", one + 2 * many, lambda: TW.fpdt_tw_experts_combine_bwd(Xs, weight, place, X[:tokens], dys, dweight)),
+                ("experts_affine_fwd", "tflops", 2.0 * sent * nm * half, lambda: TW.fpdt_tw_experts_affine_fwd(Xs, We, None, None, None, H, offsets, silu)),
+                ("experts_linear_bwd", "tflops", 4.0 * sent * nm * half, lambda: TW.fpdt_tw_experts_linear_bwd(Xs, We, H, dys, dWe, offsets))]
+    for name, unit, amount, fn in ops:
+        ms = _time(fn, iters)
+        print(json.dumps({"op": name, "rows": rows, "n_chunks": None, "ms": round(ms, 4), unit: round(amount / ms * 1e-9, 2 if unit[1] == "b" else 1)}), flush=True)
 
 
 if __name__ == "__main__":

@@ -59,8 +59,8 @@ template <int ACT> struct Epilogue {
 };
 
 // ---- few rows -------------------------------------------------------------------------------
-// The product of M <= 16 MT rows with 16 columns (rows of W) from n0 on, and what is behind it, by one workgroup of FEW_WAVES waves: a wave takes every
-// FEW_WAVES-th 64 of k, fragments straight from memory (no other workgroup reads these rows of W; those of X come from L2), and the
+// The product of M <= 16 MT rows with 16 columns (rows of W) from n0 on, and what is behind it, by one workgroup of FEW_WAVES waves: a wave takes a
+// range of k, fragments straight from memory (no other workgroup reads these rows of W; those of X come from L2), and the
 // waves' sums are added in LDS.  Bound by the memory, that is by the bytes under way: the fragments of the next U units are requested before
 // the MFMAs of these, and there is no barrier but the last.  16 rows, weights that come from HBM, us: 4096 x 4096 11.4 (tiles of 64 x 256 in 16 splits and
 // their sums 19.7), 1024 x 1024 4.3 (9.1), 2560 x 10240 20.4 (21.0), but 4096 x 14336 35.3 (29.8).  32 columns a workgroup, which read X half as often, took
@@ -70,26 +70,27 @@ template <int ACT, int MT> __device__ __forceinline__ void few_rows(float* sums,
 {
     constexpr int U = 2;  // units of 64 k
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fk = 8 * (lane >> 4);
+    // this wave's part of k, in units of 64
+    const int units = (K + 63) / 64, each = (units + FEW_WAVES - 1) / FEW_WAVES, first = wave * each, last = first + each < units ? first + each : units;
     // rows behind the operands are read as the last one: their products are not stored
-    const uint16_t *w = W + (int64_t)(n0 + fr < N ? n0 + fr : N - 1) * K + fk + 64 * wave, *x[MT];
+    const uint16_t *w = W + (int64_t)(n0 + fr < N ? n0 + fr : N - 1) * K + fk + 64 * first, *x[MT];
     floatx4 acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        x[i] = X + (int64_t)(16 * i + fr < M ? 16 * i + fr : M - 1) * K + fk + 64 * wave;
+        x[i] = X + (int64_t)(16 * i + fr < M ? 16 * i + fr : M - 1) * K + fk + 64 * first;
         acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     struct Some {
         bf16x8 a[U][2], b[U][2][MT];
     };
-    constexpr int STEP = 64 * FEW_WAVES;  // from a wave's unit to its next one
     auto fetch = [&](Some& s, int k0, auto whole_tag) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole_tag)::value;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int k = k0 + STEP * u + 32 * h;
-                const bool in = WHOLE || 64 * wave + k + fk < K;  // (K is a multiple of 8)
+                const int k = k0 + 64 * u + 32 * h;
+                const bool in = WHOLE || (64 * first + k < 64 * last && 64 * first + k + fk < K);  // (K is a multiple of 8)
                 s.a[u][h] = in ? *reinterpret_cast<const bf16x8*>(w + k) : bf16x8{};
 #pragma unroll
                 for (int i = 0; i < MT; ++i) s.b[u][h][i] = in ? *reinterpret_cast<const bf16x8*>(x[i] + k) : bf16x8{};
@@ -103,29 +104,29 @@ template <int ACT, int MT> __device__ __forceinline__ void few_rows(float* sums,
 #pragma unroll
                 for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s.a[u][h], s.b[u][h][i], acc[i], 0, 0, 0);
     };
-    const int mine = (K / 64 - wave + FEW_WAVES - 1) / FEW_WAVES, whole = mine > 0 ? mine / U : 0;  // this wave's whole units, and pairs of them
+    const int mine = (last < K / 64 ? last : K / 64) - first, whole = mine > 0 ? mine / U : 0;  // this wave's whole units, and U at a time
     Some s0, s1;
     if (whole > 0) {
         fetch(s0, 0, std::true_type{});
         int i = 0;
         for (; i + 2 < whole; i += 2) {  // (nothing is conditional in here: a wait counts what is under way)
-            fetch(s1, STEP * U * (i + 1), std::true_type{});
+            fetch(s1, 64 * U * (i + 1), std::true_type{});
             __builtin_amdgcn_sched_barrier(0);
             add(s0);
-            fetch(s0, STEP * U * (i + 2), std::true_type{});
+            fetch(s0, 64 * U * (i + 2), std::true_type{});
             __builtin_amdgcn_sched_barrier(0);
             add(s1);
         }
         if (i + 1 < whole) {
-            fetch(s1, STEP * U * (i + 1), std::true_type{});
+            fetch(s1, 64 * U * (i + 1), std::true_type{});
             add(s0);
             add(s1);
         } else {
             add(s0);
         }
     }
-    if (64 * wave + STEP * U * whole < K) {
-        fetch(s0, STEP * U * whole, std::false_type{});
+    if (first + U * whole < last) {
+        fetch(s0, 64 * U * whole, std::false_type{});
         add(s0);
     }
     // a lane has columns 4 (lane / 16) .. + 3 of row lane % 16

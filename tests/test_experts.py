@@ -356,6 +356,25 @@ def test_gpu_offsets_that_are_none():
     assert torch.equal(room[1:-1], Y)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("nm,nf,lines", [(256, 512, 9), (100, 300, 4)])
+def test_gpu_benchmark_of_the_block(monkeypatch, capsys, nm, nf, lines):
+    """Each operation is timed; of widths that experts do not take, the dense ones."""
+    import json
+    import sys
+
+    from paper_2408_16978_amd import bench_tokenwise as bench
+    common = ("--rows 64 --n-model %d --n-ffn %d --n-qkv 300 --head-dim 50 --vocab 512 --chunks 1 --iters 1" % (nm, nf)).split()
+    counts = []
+    for more in ([], ["--feed-forward"]):
+        monkeypatch.setattr(sys, "argv", ["bench"] + common + more)
+        bench.main()
+        out = [json.loads(l) for l in capsys.readouterr().out.splitlines()]
+        assert all(l["ms"] > 0 for l in out)
+        counts.append(len(out))
+    assert counts[1] - counts[0] == lines
+
+
 # ------------------------------------------------------------------ a block of them
 class Block:
     """y = x + dropout(sum_j w_j (silu(xs W1^T) * (xs W3^T)) W2^T): the buffers, and forward and backward as a training step calls them."""
