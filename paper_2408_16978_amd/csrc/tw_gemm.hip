@@ -55,11 +55,12 @@ __global__ __launch_bounds__(NTHREAD, 1) void tw_gemm_kernel(Operand A, Operand 
 {
     __shared__ __attribute__((aligned(256))) u32x4 ring[ring_bytes(WMT, WNT) / 16];
     Unit at;
-    if (!find_unit(u, at)) return;
-    const int unit_stages = at.is_part ? u.split_stages : K / STAGE_K;
-    auto part_of = [&](size_t elems) { return part + ((size_t)at.split * (unsigned)(u.tiles - u.whole) + (at.id - (unsigned)u.whole)) * elems; };
-    product_tile<TA, TB, OUT_F32, ACCUM, WMT, WNT>(ring, A, B, K, Cout, ldc, M, N, at.tile_m, at.tile_n, (int)at.split * unit_stages, unit_stages, at.is_part, part_of,
-                                                   Nothing());
+    if (__builtin_expect(find_unit(u, at), 1)) {
+        const int unit_stages = at.is_part ? u.split_stages : K / STAGE_K;
+        auto part_of = [&](size_t elems) { return part + ((size_t)at.split * (unsigned)(u.tiles - u.whole) + (at.id - (unsigned)u.whole)) * elems; };
+        product_tile<TA, TB, OUT_F32, ACCUM, WMT, WNT>(ring, A, B, K, Cout, ldc, M, N, at.tile_m, at.tile_n, (int)at.split * unit_stages, unit_stages, at.is_part, part_of,
+                                                       Nothing());
+    }
 }
 
 // The divided tiles of a product: C (+)= the sums of their splits, part [split][tile][TM x TN] fp32.

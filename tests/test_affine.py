@@ -99,7 +99,7 @@ def test_compiler_moves_no_accumulator(source, count):
         subprocess.run([lib_build.HIPCC] + lib_build.FLAGS + ["-S", "--cuda-device-only", os.path.join(lib_build.SRC_DIR, source), "-o", out], check=True, capture_output=True)
         with open(out) as f:
             text = f.read()
-    kernels = [k for k in re.findall(r"^(_ZN\S*):(.*?)^\.Lfunc_end", text, re.S | re.M) if "v_mfma" in k[1]]
+    kernels = [k for k in re.findall(r"^(_ZN\S*):(.*?)^\.Lfunc_end", text, re.S | re.M) if "global_load_lds" in k[1]]
     assert len(kernels) == count
     for name, k in kernels:
         loops = False  # from an MFMA on, until the wait
