@@ -90,10 +90,12 @@ def test_workspace_bytes_and_binding():
         TW.fpdt_tw_affine_bwd(x, None, x, x, None, None)
 
 
-@pytest.mark.parametrize("source,count", [("tw_affine.hip", 15), ("tw_experts_gemm.hip", 12), ("tw_experts_gemm_bwd.hip", 8)])
-def test_compiler_moves_no_accumulator(source, count):
+@pytest.mark.parametrize("source,count,requests", [("tw_affine.hip", 15, 15), ("tw_experts_gemm.hip", 12, 27), ("tw_experts_gemm_bwd.hip", 8, 0)])
+def test_compiler_moves_no_accumulator(source, count, requests):
     """As for the other products: from the first MFMA of a tile loop to the wait behind its last one no instruction of the compiler's may touch an accumulation
-    register, and every address that a copy takes from scalar registers is in some."""
+    register, and every address that a copy takes from scalar registers is in some.  What joins a whole tile is requested in front of the last two stages by as many
+    loads as the wait for the last copies counts: four rows of accumulator tiles of four accesses (256, 192 and 128 rows), two of four (64 rows), four of two (128 columns),
+    in one block of instructions for each tile loop."""
     with tempfile.TemporaryDirectory() as d:
         out = os.path.join(d, "x.s")
         subprocess.run([lib_build.HIPCC] + lib_build.FLAGS + ["-S", "--cuda-device-only", os.path.join(lib_build.SRC_DIR, source), "-o", out], check=True, capture_output=True)
@@ -111,6 +113,14 @@ def test_compiler_moves_no_accumulator(source, count):
             assert not (loops and ("accvgpr" in line or "scratch" in line)), (name, line)
             assert not re.match(r"s_mov_b64 s\[[0-9:]+\], v", line), (name, line)
         assert not loops, name
+    found = 0
+    for _, k in kernels:
+        lines = [x for x in (line.split(";")[0].strip() for line in k.splitlines()) if x]
+        starts = [i for i, x in enumerate(lines) if x.startswith(".LBB")] + [len(lines)]
+        for a, b in zip(starts, starts[1:]):
+            loads = sum(x.startswith("global_load_dwordx4") for x in lines[a:b])
+            found += loads in (8, 16) and not any("accvgpr_read" in x for x in lines[a:b])
+    assert found == requests
 
 
 # ------------------------------------------------------------------ parity (GPU)
