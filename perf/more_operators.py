@@ -381,7 +381,8 @@ def _own(s):
     if c["direction"] == "fwd":
         TW.fpdt_tw_affine_fwd(s["x"], s["w"], s["b"], s["r"], s["z"], s["y"], act, join, s["workspace"])
         return {"y": s["y"], "z": s["z"]}
-    TW.fpdt_tw_affine_bwd(s["z"], s["r"], s["dy"], s["dz"], s["dr"], s["db"], act, join, s["offsets"] if c["experts"] else None, s["workspace"])
+    if s["dz"] is not None or s["db"] is not None:  # (a residual alone: its gradient and the product's are dy itself, and no call is made)
+        TW.fpdt_tw_affine_bwd(s["z"], s["r"], s["dy"], s["dz"], s["dr"], s["db"], act, join, s["offsets"] if c["experts"] else None, s["workspace"])
     return {"dz": s["dz"], "dr": s["dr"], "db": s["db"]}
 
 
