@@ -53,7 +53,8 @@ template <int ACT, int MT> __global__ __launch_bounds__(FEW_WAVES * 64) void aff
 // ---- backward of what is behind a product -------------------------------------------------
 // dz = dy act'(z) (r), dr = dy act(z); the columns' sums of dz in fp32 before it is rounded.
 //
-// Bound by the memory: every tensor is read or written once, eight columns a lane.  A workgroup of `cols` x (256 / cols) threads walks the rows of its
+// Bound by the memory, and with GELU nearly by the vector instructions: every tensor is read or written once, eight columns a lane (16384 x 10240, us and TB/s: the sums alone
+// 61, 5.5, GELU with them 195, 5.2, SILU and gate 319, 5.3).  A workgroup of `cols` x (256 / cols) threads walks the rows of its
 // slice and keeps its columns' sums in registers; where an expert's rows end in the slice they are left as a row of partial sums, number slice + expert
 // (no two pairs that meet have the same number), for affine_sums_kernel: no atomics, the same order of sums in every call.
 struct Backward {

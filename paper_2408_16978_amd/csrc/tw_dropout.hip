@@ -2,7 +2,9 @@
 //
 //     y = keep x s + r,   keep by 16 bits of a counter-based generator for each element
 //
-// Bound by the memory: the generator's ten rounds of two 32 x 32 -> 64 bit products serve eight elements, and run under the accesses.
+// Bound by the memory: the generator's ten rounds of two 32 x 32 -> 64 bit products serve eight elements, and run under the accesses (65536 x 2560 in bf16 with
+// the residual: 158 us, 6.4 TB/s, vector instructions in half of the time).  Sixteen bits an element and not 32, which would take twice the rounds: p is a multiple of 2^-16,
+// and the scale that of the share that is kept.
 #include <cmath>
 
 #include "../../include/fpdt_tokenwise.h"

@@ -1,6 +1,9 @@
 // The experts' products (include/fpdt_tokenwise.h: fpdt_tw_experts_affine_fwd).
 //
 //     z = x W^T + b,   y = act(z) + r  or  act(z) r          (W, b: of the row's expert)
+//
+// Bound by the matrix cores as the dense product is (61% of the cycles; 16384 rows of 8 experts, 4096 x 14336, bare 1540 us, the dense product 1282), and with few rows
+// by the weights' bytes.  What the experts cost: rounds of tiles that are partly empty, and weights that no other rows share.
 #include "tw_experts_gemm.h"
 
 namespace fpdt_tw {

@@ -1,6 +1,9 @@
 // The products of the experts' backward (include/fpdt_tokenwise.h: fpdt_tw_experts_linear_bwd).
 //
 //     dx = dy W,   dW += dy^T x                              (for each expert's rows)
+//
+// 64 experts, 30000 rows, 2048 x 1536: dx 200 us, 0.94 PFLOP/s (24 stages of k a tile, and an epilogue each); dW 372 us, bound by its sums in fp32, 1.6 GB read and written,
+// which several workgroups a compute unit (tiles of 64 x 256 and 128 x 128) did not hide better (447 and 414).
 #include "tw_experts_gemm.h"
 
 namespace fpdt_tw {
