@@ -204,8 +204,9 @@ int fpdt_tw_norm_bwd(const void *S, const void *W, const float *stats, const voi
  *     dB[e] += sum over the rows of e of dZ                          (ACCUMULATED into the caller's fp32 [experts, n_out])
  *   Z, R, dY in; dZ, dR out: bf16 [rows, n_out].  Z, R and dR may be NULL where the formulas do not read or want them; dZ too with ACT_NONE and
  *   JOIN_ADD (where it is dY); dB may be NULL.  dZ and dR may each be Z, R or dY (not both the same).
- *   offsets: NULL with experts = 1, or int32 [experts + 1] on the device as fpdt_tw_experts_sort writes them: the rows from offsets[e] on, up to
- *   offsets[e + 1], are e's, and rows without an expert are neither read nor written.
+ *   offsets: NULL with experts = 1, or int32 [experts + 1] on the device as fpdt_tw_experts_sort writes them, or a part of those (the experts of
+ *   one group): the rows from offsets[e] on, up to offsets[e + 1], are e's, and rows without an expert, in front of the first as behind the last, are
+ *   neither read nor written.
  *   workspace (where dB is given): >= fpdt_tw_affine_bwd_workspace_bytes(...)
  * Arithmetic and sums in fp32, each output rounded once (dB: partial sums in fp32, added up in fp64); the order of the sums depends on the sizes and offsets alone.
  */

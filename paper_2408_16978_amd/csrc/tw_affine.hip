@@ -78,11 +78,11 @@ template <int ACT, bool TIMES, bool WHOLE> __global__ __launch_bounds__(256) voi
     constexpr bool BEHIND = TIMES || ACT != FPDT_TW_ACT_NONE;
     __shared__ float lds[256 * V];
     const int tc = threadIdx.x % b.cols, tr = threadIdx.x / b.cols, lines = 256 / b.cols, c = ((int)blockIdx.x * b.cols + tc) * V, left = b.n - c;
-    const int64_t used = start_of(b.offsets, b.experts, b.rows);
-    int64_t row = (int64_t)blockIdx.y * b.slice;
-    const int64_t last = row + b.slice < used ? row + b.slice : used;
+    const int64_t used = start_of(b.offsets, b.experts, b.rows), begin = start_of(b.offsets, 0, b.rows), from = (int64_t)blockIdx.y * b.slice;
+    const int64_t last = from + b.slice < used ? from + b.slice : used;
+    int64_t row = from < begin ? begin : from;  // rows in front of the first expert's are nobody's
     int e = 0;
-    for (int up = b.experts; up - e > 1;) {  // the last expert that begins at or before the slice
+    for (int up = b.experts; up - e > 1;) {  // the last expert that begins at or before this row
         const int mid = (e + up) / 2;
         if (start_of(b.offsets, mid, b.rows) <= row) e = mid;
         else up = mid;

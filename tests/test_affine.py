@@ -413,3 +413,40 @@ def test_gpu_two_streams_and_captured():
     step(a)
     torch.cuda.synchronize()
     assert all(torch.equal(a[k], t[k]) for t in (b, c) for k in ("Y", "Z", "dZ", "dR", "dB"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_out", [40, 2056, 77])
+@pytest.mark.parametrize("counts,first", [([5, 40, 0, 60], 10), ([5, 40, 0, 60], 16), ([0, 0, 30, 1], 64), ([70, 0, 90], 100), ([1] * 50, 130), ([0, 0], 30), ([100], 7), ([64], 64)])
+def test_gpu_backward_of_experts_that_begin_behind_other_rows(n_out, counts, first):
+    """A part of sorted offsets, the first of them not 0: within a slice of rows (64 of them at 40 and 77 columns, 16 at 2056), at its end, some slices in.  The rows in front
+    (and behind) are another's: not read (they hold NaN), not written, in no sum."""
+    E, used = len(counts), sum(counts)
+    ends = first + np.concatenate([[0], np.cumsum(counts)])
+    rows = first + used + 9
+    g = torch.Generator(device="cuda").manual_seed(first)
+    Z, R, dY = ((torch.randn(rows, n_out, device="cuda", generator=g) * s).to(torch.bfloat16) for s in (2.0, 1.0, 0.1))
+    every = torch.tensor([0, first // 2] + list(ends) + [rows], dtype=torch.int32, device="cuda")  # (those of all experts)
+    offsets, mine = every[2:-1], slice(first, first + used)
+    ref = otw.affine_behind_bwd(f64(Z), f64(R), f64(dY), "gelu", True)
+    raw, tz, _ = budget_bwd(Z, R, dY, ref, "gelu", True, 64)
+    plain = f64(dY)
+    for t in (Z, R, dY):
+        t[:first], t[first + used:] = float("nan"), float("nan")
+    ws = torch.empty(TW.fpdt_tw_affine_bwd_workspace_bytes(rows, n_out, E), dtype=torch.uint8, device="cuda")
+    dZ, dR = torch.full_like(dY, 9.0), torch.full_like(dY, 9.0)
+    dB = torch.randn(E, n_out, device="cuda", generator=g)
+    sums, was = dB.clone(), f64(dB)
+    TW.fpdt_tw_affine_bwd(Z, R, dY, dZ, dR, dB, ACT["gelu"], TW.FPDT_TW_JOIN_TIMES, offsets, ws)
+    TW.fpdt_tw_affine_bwd(None, None, dY, None, None, sums, offsets=offsets, workspace=ws)
+    torch.cuda.synchronize()
+    _close("dZ", dZ[mine], ref["dZ"][mine], tz[mine] + 2.0 ** -126)
+    _close("dR", dR[mine], ref["dR"][mine], (HALF + 2.0 ** -19) * np.abs(ref["dR"][mine]) + 2.0 ** -126)
+    for t in (dZ, dR):
+        assert (t[:first] == 9).all() and (t[first + used:] == 9).all()
+    for e in range(E):
+        part = slice(ends[e], ends[e + 1])
+        want = was[e] + ref["dZ"][part].sum(axis=0)
+        _close("dB", dB[e], want, raw[part].sum(axis=0) + 98 * 2.0 ** -24 * np.abs(ref["dZ"][part]).sum(axis=0) + 2.0 ** -24 * np.abs(want))
+        want = was[e] + plain[part].sum(axis=0)
+        _close("sums alone", sums[e], want, 98 * 2.0 ** -24 * np.abs(plain[part]).sum(axis=0) + 2.0 ** -24 * np.abs(want))
