@@ -299,15 +299,15 @@ int check_rows(int64_t rows, int top, int hidden, int dtype)
     if (rows > INT32_MAX || rows * top > INT32_MAX || hidden > 1 << 28) return fail(TW_UNSUPPORTED, "sizes beyond the launch limits");
     return TW_OK;
 }
-// Nothing that is written meets anything else, but where it is the very tensor `same`.
+// Nothing that is written meets anything else, but where it is the very tensor number `same` of `in` (and that alone).
 struct Arg {
     const void* p;
     size_t bytes;
 };
-bool meets(const Arg& out, const Arg* in, int n, const void* same = nullptr)
+bool meets(const Arg& out, const Arg* in, int n, int same = -1)
 {
     for (int i = 0; i < n; ++i)
-        if (out.p && in[i].p && !(in[i].p == out.p && out.p == same) && ranges_meet(out.p, out.bytes, in[i].p, in[i].bytes)) return true;
+        if (out.p && in[i].p && !(i == same && in[i].p == out.p) && ranges_meet(out.p, out.bytes, in[i].p, in[i].bytes)) return true;
     return false;
 }
 // f(element type, WHOLE)
@@ -340,7 +340,7 @@ int gathered_sum(const void* In, const float* weight, const int32_t* place, cons
     if (misaligned(In, size) || misaligned(R, size) || misaligned(Out, size) || misaligned(place, 4) || misaligned(weight, 4))
         return fail(TW_INVALID, "a tensor is not aligned to its elements");
     const Arg in[] = {{In, one * top}, {weight, index}, {place, index}, {R, one}};
-    if (meets({Out, one}, in, 4, R)) return fail(TW_INVALID, "the output overlaps another tensor");
+    if (meets({Out, one}, in, 4, 3)) return fail(TW_INVALID, "the output overlaps another tensor");
     const Rows s = {place, weight, rows, rows * top, top, hidden};
     const int chunks = chunks_of(hidden);
     by_type(dtype, hidden, [&](auto type, auto whole) {
@@ -435,7 +435,7 @@ int fpdt_tw_experts_combine_bwd(const void* Ys, const float* weight, const int32
     if (misaligned(Ys, size) || misaligned(dY, size) || misaligned(dYs, size) || misaligned(place, 4) || misaligned(weight, 4) || misaligned(dweight, 4))
         return fail(TW_INVALID, "a tensor is not aligned to its elements");
     const Arg in[] = {{Ys, one * top}, {weight, index}, {place, index}, {dY, one}, {dYs, one * top}};
-    if (meets({dYs, one * top}, in, 4, Ys) || meets({dweight, index}, in, 5)) return fail(TW_INVALID, "dYs or dweight overlaps another tensor");
+    if (meets({dYs, one * top}, in, 4, 0) || meets({dweight, index}, in, 5)) return fail(TW_INVALID, "dYs or dweight overlaps another tensor");
     const Rows s = {place, weight, rows, rows * top, top, hidden};
     const int tokens = top < SMALL / 64 ? SMALL / 64 / top : 1;
     hipStream_t st = static_cast<hipStream_t>(stream);

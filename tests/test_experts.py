@@ -485,3 +485,16 @@ def test_gpu_blocks_on_two_streams():
         torch.cuda.synchronize()
         for name in Block.OUT:
             assert torch.equal(getattr(a, name), getattr(b, name)), name
+
+
+@pytest.mark.parametrize("top", [1, 2])
+def test_one_tensor_in_three_places_is_refused(top):
+    """An output may be the residual, or Ys, and nothing else with it: rows are read by place and written by token (or the other way round), so a tensor that is all three
+    would be read by some workgroups behind what others wrote."""
+    a, b, c, d = PTRS["a"], PTRS["b"], PTRS["c"], PTRS["d"]
+    sizes = (64, top, 64, 1)
+    assert L("gather_bwd")(a, c, a, a, *sizes, None) == 1 and TW.fpdt_tw_last_error() != ""
+    assert L("combine_fwd")(a, b, c, a, a, *sizes, None) == 1 and TW.fpdt_tw_last_error() != ""
+    assert L("combine_fwd")(d, a, c, a, a, *sizes, None) == 1 and L("combine_fwd")(d, b, a, a, a, *sizes, None) == 1
+    assert L("combine_bwd")(a, b, c, a, a, None, *sizes, None) == 1 and TW.fpdt_tw_last_error() != ""
+    assert L("combine_bwd")(a, a, c, d, a, None, *sizes, None) == 1 and L("combine_bwd")(a, b, a, d, a, None, *sizes, None) == 1
