@@ -227,48 +227,51 @@ template <class T, bool WEIGHTED, bool WHOLE> __global__ __launch_bounds__(SMALL
 
 // dys[place(t, j)] = w(t, j) dy[t],  dw(t, j) = dy[t] . ys[place(t, j)].  (10007 tokens of 2560 in bf16, eight places: 157-165 us, 5.3 TB/s; eight waves a
 // workgroup 160; ys through the caches 174.)  A wave takes an assignment at a time, a workgroup those of `tokens` neighbouring
-// tokens, so that a row of dy comes from the memory once.
+// tokens, so that a row of dy comes from the memory once.  (The grid is bounded as the others' are: of a launch of 2^32 threads and more, those beyond
+// do not run, without an error.)
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(SMALL) void combine_bwd_kernel(const T* Ys, const T* dY, T* dYs, float* dweight, Rows s, int tokens)
 {
     constexpr int V = 16 / sizeof(T), CHUNK = chunk_of<T>;
     const int lane = threadIdx.x & 63;
-    const int64_t first = (int64_t)blockIdx.x * tokens * s.top, end = first + (int64_t)tokens * s.top, last = end < s.rows * s.top ? end : s.rows * s.top;
-    for (int64_t a = first + wave_id(); a < last; a += SMALL / 64) {
-        const int64_t t = a / s.top, p = place_of(s, a);
-        if (p < 0) {
-            if (dweight && lane == 0) dweight[a] = 0.f;
-            continue;
-        }
-        const float w = dYs ? s.weight[a] : 0.f;
-        float dot = 0.f;
-        for (int c0 = lane * V; c0 < s.hidden; c0 += CHUNK * 64 * V) {
-            Vec<T, V> dy[CHUNK], y[CHUNK];
-#pragma unroll
-            for (int k = 0; k < CHUNK; ++k) {
-                const int c = c0 + k * 64 * V;
-                if (c >= s.hidden) continue;
-                dy[k] = take<WHOLE, V>(dY + t * s.hidden, c, s.hidden, false);
-                if (dweight) y[k] = take<WHOLE, V>(Ys + p * s.hidden, c, s.hidden, true);
+    for (int64_t token = (int64_t)blockIdx.x * tokens; token < s.rows; token += (int64_t)gridDim.x * tokens) {
+        const int64_t first = token * s.top, end = first + (int64_t)tokens * s.top, last = end < s.rows * s.top ? end : s.rows * s.top;
+        for (int64_t a = first + wave_id(); a < last; a += SMALL / 64) {
+            const int64_t t = a / s.top, p = place_of(s, a);
+            if (p < 0) {
+                if (dweight && lane == 0) dweight[a] = 0.f;
+                continue;
             }
+            const float w = dYs ? s.weight[a] : 0.f;
+            float dot = 0.f;
+            for (int c0 = lane * V; c0 < s.hidden; c0 += CHUNK * 64 * V) {
+                Vec<T, V> dy[CHUNK], y[CHUNK];
 #pragma unroll
-            for (int k = 0; k < CHUNK; ++k) {
-                const int c = c0 + k * 64 * V;
-                if (c >= s.hidden) continue;
-                if (dweight)
+                for (int k = 0; k < CHUNK; ++k) {
+                    const int c = c0 + k * 64 * V;
+                    if (c >= s.hidden) continue;
+                    dy[k] = take<WHOLE, V>(dY + t * s.hidden, c, s.hidden, false);
+                    if (dweight) y[k] = take<WHOLE, V>(Ys + p * s.hidden, c, s.hidden, true);
+                }
 #pragma unroll
-                    for (int e = 0; e < V; ++e) dot = fmaf(to_float(dy[k].e[e]), to_float(y[k].e[e]), dot);
-                if (dYs) {
-                    float d[V];
+                for (int k = 0; k < CHUNK; ++k) {
+                    const int c = c0 + k * 64 * V;
+                    if (c >= s.hidden) continue;
+                    if (dweight)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) d[e] = w * to_float(dy[k].e[e]);
-                    give<WHOLE, V>(dYs + p * s.hidden, c, s.hidden, rounded<V>(d, T()));
+                        for (int e = 0; e < V; ++e) dot = fmaf(to_float(dy[k].e[e]), to_float(y[k].e[e]), dot);
+                    if (dYs) {
+                        float d[V];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) d[e] = w * to_float(dy[k].e[e]);
+                        give<WHOLE, V>(dYs + p * s.hidden, c, s.hidden, rounded<V>(d, T()));
+                    }
                 }
             }
-        }
-        if (dweight) {
-            dot = lanes_sum<64>(dot);
-            if (lane == 0) dweight[a] = dot;
+            if (dweight) {
+                dot = lanes_sum<64>(dot);
+                if (lane == 0) dweight[a] = dot;
+            }
         }
     }
 }
@@ -438,11 +441,13 @@ int fpdt_tw_experts_combine_bwd(const void* Ys, const float* weight, const int32
     if (meets({dYs, one * top}, in, 4, 0) || meets({dweight, index}, in, 5)) return fail(TW_INVALID, "dYs or dweight overlaps another tensor");
     const Rows s = {place, weight, rows, rows * top, top, hidden};
     const int tokens = top < SMALL / 64 ? SMALL / 64 / top : 1;
+    const int64_t groups = (rows + tokens - 1) / tokens;
+    const unsigned grid = (unsigned)(groups < 1 << 20 ? groups : 1 << 20);
     hipStream_t st = static_cast<hipStream_t>(stream);
     by_type(dtype, hidden, [&](auto type, auto whole) {
         typedef decltype(type) T;
-        combine_bwd_kernel<T, decltype(whole)::value><<<(unsigned)((rows + tokens - 1) / tokens), SMALL, 0, st>>>(static_cast<const T*>(Ys), static_cast<const T*>(dY),
-                                                                                                                   static_cast<T*>(dYs), dweight, s, tokens);
+        combine_bwd_kernel<T, decltype(whole)::value><<<grid, SMALL, 0, st>>>(static_cast<const T*>(Ys), static_cast<const T*>(dY), static_cast<T*>(dYs), dweight, s,
+                                                                              tokens);
     });
     HIP_TRY(hipGetLastError());
     return TW_OK;

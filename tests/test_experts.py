@@ -498,3 +498,51 @@ def test_one_tensor_in_three_places_is_refused(top):
     assert L("combine_fwd")(d, a, c, a, a, *sizes, None) == 1 and L("combine_fwd")(d, b, a, a, a, *sizes, None) == 1
     assert L("combine_bwd")(a, b, c, a, a, None, *sizes, None) == 1 and TW.fpdt_tw_last_error() != ""
     assert L("combine_bwd")(a, a, c, d, a, None, *sizes, None) == 1 and L("combine_bwd")(a, b, a, d, a, None, *sizes, None) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,top", [((1 << 24) + 5, 4), ((1 << 26) + 3, 1), (3000001, 6), (5000011, 2)])
+def test_gpu_more_rows_than_one_turn_of_a_grid(rows, top):
+    """Narrow rows, more of them than the largest grid has waves (2^22) or workgroups (2^20), and more than a launch takes (2^32 threads; one of more is cut off without an error): small whole numbers, weights of
+    1/2, 1 and 2, so that every product and sum is exact."""
+    hidden = 8
+    g = torch.Generator(device="cuda").manual_seed(top)
+    taken = lambda t, index: torch.cat([t[i] for i in index.split(1 << 22)])  # (one index call of torch's over 2^26 rows and more is cut off at that)
+    small = lambda n: torch.randint(-8, 9, (n, hidden), device="cuda", generator=g, dtype=torch.int8).to(torch.bfloat16)
+    place = torch.randperm(rows * top, device="cuda", generator=g, dtype=torch.int32).view(rows, top)
+    place[::7, 0] = -1
+    there = (place >= 0)[..., None]
+    at = place.clamp(min=0).long()
+    X, R, Ys = small(rows), small(rows), small(rows * top)
+    weight = torch.randint(-1, 2, (rows, top), device="cuda", generator=g).float().exp2()
+    print("[case] rows of several turns", rows, top, flush=True)
+    # to their places
+    Xs = torch.full_like(Ys, 9.0)
+    TW.fpdt_tw_experts_gather_fwd(X, place, Xs)
+    want = torch.full_like(Ys, 9.0)
+    for j in range(top):
+        sent = there[:, j, 0]
+        want[at[sent, j]] = taken(X, sent.nonzero()[:, 0])
+    assert torch.equal(Xs, want)
+    del Xs, want
+    # and back
+    Y, Y2 = torch.full_like(X, float("nan")), torch.full_like(X, float("nan"))
+    TW.fpdt_tw_experts_combine_fwd(Ys, weight, place, R, Y)
+    TW.fpdt_tw_experts_gather_bwd(Ys, place, None, Y2)
+    total, plain = R.float(), torch.zeros(rows, hidden, device="cuda")
+    for j in range(top):
+        y = torch.where(there[:, j], taken(Ys, at[:, j]).float(), 0.0)
+        total += y * weight[:, j, None]
+        plain += y
+    assert torch.equal(Y.float(), total) and torch.equal(Y2.float(), plain)
+    del Y, Y2, total, plain
+    # the gradient
+    dYs, dweight = torch.full_like(Ys, 9.0), torch.full_like(weight, float("nan"))
+    TW.fpdt_tw_experts_combine_bwd(Ys, weight, place, X, dYs, dweight)
+    want = torch.full_like(Ys, 9.0)
+    for j in range(top):
+        sent = there[:, j, 0]
+        want[at[sent, j]] = (taken(X, sent.nonzero()[:, 0]).float() * weight[sent, j, None]).bfloat16()
+        dots = torch.where(sent, (X.float() * taken(Ys, at[:, j]).float()).sum(1), 0.0)
+        assert torch.equal(dweight[:, j], dots)
+    assert torch.equal(dYs, want)
