@@ -270,7 +270,8 @@ int fpdt_tw_experts_combine_bwd(const void *Ys, const float *weight, const int32
  *     dX = dY W[e]   (written, bf16; NULL to skip),   dW[e] += dY^T X over e's rows   (ACCUMULATED, fp32; NULL to skip)
  *   X, dX [rows, n_in], R, Z, Y, dY [rows, n_out] in the order of the sort; rows from offsets[experts] on are neither read nor written.  offsets may say
  *   anything: rows outside [0, rows) are not touched.  Y may be R.
- *   n_in and n_out multiples of 8, X, W and dY 16-byte aligned, experts <= 1024.  No workspace.
+ *   n_in and n_out multiples of 8, X, W and dY 16-byte aligned, experts <= 1024, at most 2^24 - 8 tiles of 256 x 256 or less (an expert's rows and columns, for dW its
+ *   n_out and n_in, each rounded up).  No workspace.
  */
 int fpdt_tw_experts_affine_fwd(const void *X, const void *W, const void *B, const void *R, void *Z, void *Y,
                                const int32_t *offsets, int64_t rows, int experts, int n_in, int n_out, int act, int join,

@@ -19,16 +19,17 @@ struct Groups {
 struct GroupTile {
     int expert, first, rows, tile_m, tile_n;
 };
+__device__ __forceinline__ unsigned tiles_of(int rows, int tm) { return ((unsigned)rows + (unsigned)tm - 1) / (unsigned)tm; }
 __device__ __forceinline__ bool find_group(const Groups& g, int tm, unsigned tiles_n, GroupTile& at)
 {
     // a lane counts the tile rows of `per` neighbouring experts, of which it keeps the first one's rows
     const int lane = threadIdx.x & 63, per = (g.experts + 63) / 64, e0 = lane * per;
     auto begin_of = [&](int e) { return offset_of(g.offsets, e < g.experts ? e : g.experts, g.rows); };
     const int own = begin_of(e0), next = begin_of(e0 + 1), own_rows = next > own ? next - own : 0;
-    unsigned mine = (unsigned)(own_rows + tm - 1) / (unsigned)tm;
+    unsigned mine = tiles_of(own_rows, tm);
     for (int i = 1, from = next; i < per; ++i) {
         const int to = begin_of(e0 + i + 1);
-        mine += to > from ? (unsigned)(to - from + tm - 1) / (unsigned)tm : 0u;
+        mine += to > from ? tiles_of(to - from, tm) : 0u;
         from = to;
     }
     unsigned upto = mine;  // those of the lanes up to this one
@@ -43,13 +44,13 @@ __device__ __forceinline__ bool find_group(const Groups& g, int tm, unsigned til
     const int owner = __builtin_ctzll(__ballot(upto * tiles_n > id));
     unsigned base = (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), owner);
     int e = owner * per, first = __builtin_amdgcn_readlane(own, owner), rows = __builtin_amdgcn_readlane(own_rows, owner);
-    unsigned tiles = (unsigned)(rows + tm - 1) / (unsigned)tm;
+    unsigned tiles = tiles_of(rows, tm);
     while ((base + tiles) * tiles_n <= id && e + 1 < g.experts) {  // (not with 64 experts and fewer)
         base += tiles;
         first = begin_of(++e);
         const int end = begin_of(e + 1);
         rows = end > first ? end - first : 0;
-        tiles = (unsigned)(rows + tm - 1) / (unsigned)tm;
+        tiles = tiles_of(rows, tm);
     }
     if (id - base * tiles_n >= tiles * tiles_n) return false;  // (offsets that do not ascend)
     at.expert = (int)fpdt::uniform((unsigned)e);
@@ -79,8 +80,10 @@ template <int WMT, class F> __device__ __forceinline__ void by_rows(int left, F 
 // rows, 4096 x 14336, 191 and 161; 8 of 250 rows, 1024 x 1024, 25 and 14, of 128 x 128 11.
 struct GroupPlan {
     int wmt, wnt;
-    int64_t tiles;  // at most, whatever the offsets
+    int64_t tiles;  // at most, whatever the offsets; 0: more in every tile than a launch has
 };
+// Of a launch of 2^32 threads and more, those beyond do not run, without an error.  (A grid is rounded up to a multiple of 8.)
+constexpr int64_t MOST_TILES = ((int64_t)1 << 32) / NTHREAD - 8;
 double tile_clocks(int wm, int wn, bool two, int steps)
 {
     const double mfma = two ? 161. * wm * wn + 158. : 64. * wm * wn + 116., copies = (two ? 175. : 85.) * (wm + wn);
@@ -95,7 +98,8 @@ GroupPlan plan_groups(int64_t rows, int experts, int N, int K)
     const int steps = (K < SK ? SK : K) / SK;
     for (const auto& sh : shapes) {
         const bool two = sh[0] * sh[1] <= 4;
-        const int64_t tiles_n = (N + 64 * sh[1] - 1) / (64 * sh[1]), tm = 64 * sh[0];
+        const int64_t tiles_n = (N + 64 * sh[1] - 1) / (64 * sh[1]), tm = 64 * sh[0], tiles = (rows / tm + busy) * tiles_n;
+        if (tiles > MOST_TILES) continue;
         double n = 0, work = 0;
         for (int k = 0; k < 5; ++k) {
             const double some = (0.6 + 0.2 * k) * (double)rows / (double)busy;
@@ -105,7 +109,7 @@ GroupPlan plan_groups(int64_t rows, int experts, int N, int K)
             work += share * ((double)(r / tm) * tile_clocks(sh[0], sh[1], two, steps) + (last > 0 ? tile_clocks((int)((last + 63) / 64), sh[1], two, steps) : 0));
         }
         const double rounds = n / (two ? 512 : 256), c = work / n * (rounds < 3 ? std::ceil(rounds) : rounds + 0.5) * (two && n <= 256 ? 0.56 : 1.);
-        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], (rows / tm + busy) * tiles_n}, best_cost = c;
+        if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], tiles}, best_cost = c;
     }
     return best;
 }

@@ -71,7 +71,7 @@ int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, cons
     const int same[][2] = {{3, 5}};
     if ((rc = check_apart(args, 7, same, 1)) != TW_OK) return rc;
     const GroupPlan plan = plan_groups(rows, experts, n_out, n_in);
-    if (plan.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+    if (plan.tiles == 0) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
     const Groups g = {offsets, experts, (int)rows};
     hipStream_t st = static_cast<hipStream_t>(stream);
     by_act(act, [&](auto a) {

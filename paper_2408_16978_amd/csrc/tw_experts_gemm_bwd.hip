@@ -52,6 +52,7 @@ GroupPlan plan_weights(int64_t rows, int experts, int n_in, int n_out)
     const int64_t busy = rows < experts ? rows : experts, K = (rows + busy - 1) / busy;
     for (const auto& sh : shapes) {
         const int64_t each = (int64_t)((n_in + 64 * sh[1] - 1) / (64 * sh[1])) * ((n_out + 64 * sh[0] - 1) / (64 * sh[0])), tiles = each * busy;
+        if (each * experts > MOST_TILES) continue;
         const int slots = sh[0] * sh[1] <= 4 ? 512 : 256;
         const double c = launch_cost(sh[0], sh[1], (double)(tiles / slots * slots), (double)(tiles % slots), 1, (int)((K < SK ? SK : K) / SK));
         if (best_cost == 0 || c < best_cost) best = {sh[0], sh[1], each * experts}, best_cost = c;
@@ -80,7 +81,7 @@ int fpdt_tw_experts_linear_bwd(const void* X, const void* W, const void* dY, voi
                         {"dX", dX, (size_t)rows * n_in * 2, true}, {"dW", dW, weights * 4, true}, {"offsets", offsets, (size_t)(experts + 1) * 4, false}};
     if ((rc = check_apart(args, 6, nullptr, 0)) != TW_OK) return rc;
     const GroupPlan px = plan_groups(rows, experts, n_in, n_out), pw = plan_weights(rows, experts, n_in, n_out);
-    if (px.tiles > (int64_t)1 << 30 || pw.tiles > (int64_t)1 << 30) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
+    if ((dX && px.tiles == 0) || (dW && pw.tiles == 0)) return fail(TW_UNSUPPORTED, "product beyond the launch limits");
     const Groups g = {offsets, experts, (int)rows};
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto t = [](const void* p) { return static_cast<const uint16_t*>(p); };

@@ -546,3 +546,50 @@ def test_gpu_more_rows_than_one_turn_of_a_grid(rows, top):
         dots = torch.where(sent, (X.float() * taken(Ys, at[:, j]).float()).sum(1), 0.0)
         assert torch.equal(dweight[:, j], dots)
     assert torch.equal(dYs, want)
+
+
+def test_more_tiles_than_a_launch_has_are_refused():
+    """1024 experts of 2^22 columns are 2^24 tiles in any of their shapes: workgroups of 256 threads, 2^32 in all, of which none beyond that would run."""
+    far = {k: (i + 1) << 42 for i, k in enumerate("abcdefg")}
+    sizes = dict(rows=1024, experts=1024)
+    order = ("X", "W", "B", "R", "Z", "Y", "offsets", "rows", "experts", "n_in", "n_out", "act", "join")
+    base = dict(X=far["a"], W=far["b"], B=None, R=None, Z=None, Y=far["c"], offsets=far["d"], n_in=8, n_out=1 << 22, act=0, join=0, **sizes)
+    assert _call("affine_fwd", order, base) == 2 and TW.fpdt_tw_last_error() != ""
+    back = ("X", "W", "dY", "dX", "dW", "offsets", "rows", "experts", "n_in", "n_out")
+    base = dict(X=far["a"], W=far["b"], dY=far["c"], dX=None, dW=None, offsets=far["d"], **sizes)
+    assert _call("linear_bwd", back, base, dX=far["e"], n_in=1 << 22, n_out=8) == 2
+    for n_in, n_out in ((8, 1 << 22), (1 << 22, 8)):
+        assert _call("linear_bwd", back, base, dW=far["f"], n_in=n_in, n_out=n_out) == 2 and TW.fpdt_tw_last_error() != ""
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [(2 ** 31 - 1,), (2 ** 30, 0, 5, 2 ** 29 + 77, 2 ** 28, 2 ** 27 - 100)])
+def test_gpu_products_of_as_many_rows_as_there_may_be(counts):
+    """Narrow rows, 2^31 - 1 of them: tiles of 256 rows where those of 128 would be more than a launch has.  Small whole numbers, so that the products are exact."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 120 GB")
+    rows, E, n = 2 ** 31 - 1, len(counts), 8
+    ends = np.concatenate([[0], np.cumsum(counts)])
+    offsets = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(E)
+    small = lambda *s: torch.randint(-4, 5, s, device="cuda", generator=g, dtype=torch.int8).to(torch.bfloat16)
+    period = (1 << 22) + 9
+    some, W = small(period, n), small(E, n, n)
+    X, Y = torch.empty(rows, n, dtype=torch.bfloat16, device="cuda"), torch.full((rows, n), 9.0, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, period):
+        X[r:r + period] = some[:min(period, rows - r)]
+    print("[case] as many rows as there may be", counts, flush=True)
+    for back in (False, True):
+        if back:  # dX, with X for dY
+            got = torch.full_like(Y, 9.0)
+            TW.fpdt_tw_experts_linear_bwd(Y, W, X, got, None, offsets)
+        else:
+            got = Y
+            TW.fpdt_tw_experts_affine_fwd(X, W, None, None, None, got, offsets)
+        torch.cuda.synchronize()
+        by_expert = [(some.float() @ (W[e].float() if back else W[e].float().t())).bfloat16() for e in range(E)]
+        for e in range(E):
+            for r in range(int(ends[e]) // period * period, int(ends[e + 1]), period):
+                a, b = max(r, int(ends[e])), min(r + period, int(ends[e + 1]))
+                assert a >= b or torch.equal(got[a:b], by_expert[e][a - r:b - r]), (back, e, a)
+        assert (got[int(ends[-1]):] == 9).all()
