@@ -593,3 +593,40 @@ def test_gpu_products_of_as_many_rows_as_there_may_be(counts):
                 a, b = max(r, int(ends[e])), min(r + period, int(ends[e + 1]))
                 assert a >= b or torch.equal(got[a:b], by_expert[e][a - r:b - r]), (back, e, a)
         assert (got[int(ends[-1]):] == 9).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts,first,n_in,n_out", [([3, 0, 70, 17], 5, 72, 40), ([65, 130, 1], 64, 136, 264), ([300, 257, 190], 33, 200, 4104), ([4, 0, 9, 16], 7, 1032, 136)])
+def test_gpu_group_of_experts_between_rows_that_are_not_finite(counts, first, n_in, n_out):
+    """A part of sorted offsets, the first of them not 0, and NaN in the rows around them and in those of one of the experts: forward (tiles and few rows), dX and dW of the others are what they
+    are on their own, and the rows around stay as they were."""
+    import test_affine
+    E, used = len(counts), sum(counts)
+    rows, ends = first + used + 6, first + np.concatenate([[0], np.cumsum(counts)])
+    every = torch.tensor([0] + list(ends) + [rows], dtype=torch.int32, device="cuda")
+    offsets = every[1:-1]
+    g = torch.Generator(device="cuda").manual_seed(n_in)
+    bf = lambda *s, std=1.0: (torch.randn(*s, device="cuda", generator=g) * std).to(torch.bfloat16)
+    X, W, B, R, dY = bf(rows, n_in), bf(E, n_out, n_in, std=n_in ** -0.5), bf(E, n_out), bf(rows, n_out), bf(rows, n_out, std=0.1)
+    bad = slice(int(ends[E - 2]), int(ends[E - 1]))  # the last but one
+    for t in (X, R, dY):
+        t[:first], t[first + used:], t[bad] = float("nan"), float("inf"), float("nan")
+    print("[case] group of experts", counts, first, n_in, n_out, flush=True)
+    Y, Z = (torch.full((rows, n_out), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    TW.fpdt_tw_experts_affine_fwd(X, W, B, R, Z, Y, offsets, ACT["silu"], TW.FPDT_TW_JOIN_TIMES)
+    dX, dW = torch.full_like(X, 9.0), torch.zeros(E, n_out, n_in, device="cuda")
+    TW.fpdt_tw_experts_linear_bwd(X, W, dY, dX, dW, offsets)
+    torch.cuda.synchronize()
+    for t in (Y, Z, dX):
+        assert (t[:first] == 9).all() and (t[first + used:] == 9).all()
+    for e in range(E):
+        at = slice(int(ends[e]), int(ends[e + 1]))
+        if at == bad:
+            assert torch.isnan(Y[at]).all() and torch.isnan(dX[at]).all()
+            continue
+        y, ty, z, tz = test_affine.reference(X[at], W[e], B[e], R[at], "silu", True)
+        assert bool(((Y[at].double() - y).abs() <= ty).all()) and bool(((Z[at].double() - z).abs() <= tz).all()), e
+        x, d, w = X[at].double(), dY[at].double(), W[e].double()
+        want = d @ w
+        assert bool(((dX[at].double() - want).abs() <= (n_out + 2) * 2.0 ** -24 * (d.abs() @ w.abs()) + 2.0 ** -8 * want.abs()).all()), e
+        assert bool(((dW[e].double() - d.t() @ x).abs() <= (counts[e] + 2) * 2.0 ** -24 * (d.abs().t() @ x.abs())).all()), e
