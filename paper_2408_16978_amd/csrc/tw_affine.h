@@ -62,9 +62,10 @@ template <int ACT> struct Epilogue {
 // The product of M <= 16 MT rows with 16 columns (rows of W) from n0 on, and what is behind it, by one workgroup of FEW_WAVES waves: a wave takes a
 // range of k, fragments straight from memory (no other workgroup reads these rows of W; those of X come from L2), and the
 // waves' sums are added in LDS.  Bound by the memory, that is by the bytes under way: the fragments of the next U units are requested before
-// the MFMAs of these, and there is no barrier but the last.  16 rows, weights that come from HBM, us: 4096 x 4096 11.4 (tiles of 64 x 256 in 16 splits and
-// their sums 19.7), 1024 x 1024 4.3 (9.1), 2560 x 10240 20.4 (21.0), but 4096 x 14336 35.3 (29.8).  32 columns a workgroup, which read X half as often, took
-// 15.5, 5.1, 21.7 and 30.9; loads of W past the caches, which fetch a line for each half of it, 11.6, 4.5, 22.7 and 36.9.
+// the MFMAs of these, and there is no barrier but the last.  16 rows (n_in x n_out), 1 GB of weights in turn, so that they come from HBM, us: 4096 x 4096 10.8-11.4
+// (tiles of 64 x 256 in 16 splits and their sums 19.7; 3.1 TB/s of weights), 1024 x 1024 4.6 (10.5), 2560 x 10240 20.7 (22.1), but 4096 x 14336 35.6 (34.2).  Over three
+// sets in turn, which the caches hold in part, 32 columns a workgroup, which read X half as often, took 15.5 for 11.4, 5.1 for 4.3, 21.7 for 20.4 and 30.9 for 35.3; loads
+// of W past the caches, which fetch a line for each half of it, 11.6, 4.5, 22.7 and 36.9.
 constexpr int FEW_WAVES = 8, FEW_ROWS = 64, FEW_COLS = 16;
 template <int ACT, int MT> __device__ __forceinline__ void few_rows(float* sums, const uint16_t* X, const uint16_t* W, int K, int M, int N, int n0, const Epilogue<ACT>& behind)
 {
@@ -141,8 +142,9 @@ template <int ACT, int MT> __device__ __forceinline__ void few_rows(float* sums,
         if (m < M && n < N) behind.four(v, m, n, N);
     }
 }
-// Every 16 columns read X anew: it pays while that is not much.  Measured, us, few_rows and tiles: 1 row, 4096 x 14336 24.8 and 31.2; 32 rows, 4096 x 4096 15.0 and 19.1,
-// 14336 x 4096 44.7 and 33.1; 64 rows, 1024 x 1024 7.0 and 9.2, 4096 x 4096 22.7 and 19.3; 16 rows, 14336 x 4096 31.7 and 33.8, 4096 x 14336 35.3 and 29.8.
+// Every 16 columns read X anew: it pays while that is not much.  Measured with weights from HBM, us, few_rows and tiles: 1 row, 4096 x 14336 25.7 and 31.6; 32 rows, 4096 x
+// 4096 14.3 and 19.4, 14336 x 4096 44.9 and 36.3; 64 rows, 1024 x 1024 7.4 and 11.0, 4096 x 4096 22.4 and 19.8; 16 rows, 14336 x 4096 34.9 and 36.2, 4096 x 14336 35.6 and
+// 34.2.
 inline bool few_pays(int64_t rows, int64_t weights) { return rows * weights <= (int64_t)16 * 34 << 20; }
 template <int MT> constexpr int few_lds = FEW_WAVES * MT * 64 * 4;  // floats
 

@@ -3,7 +3,7 @@
 //     y = keep x s + r,   keep by 16 bits of a counter-based generator for each element
 //
 // Bound by the memory: the generator's ten rounds of two 32 x 32 -> 64 bit products serve eight elements, and run under the accesses (65536 x 2560 in bf16 with
-// the residual: 158 us, 6.4 TB/s, vector instructions in half of the time).  Sixteen bits an element and not 32, which would take twice the rounds: p is a multiple of 2^-16,
+// the residual: 157-159 us between events around many calls, 6.3-6.4 TB/s; 162-168 in a kernel trace; vector instructions in half of the time).  Sixteen bits an element and not 32, which would take twice the rounds: p is a multiple of 2^-16,
 // and the scale that of the share that is kept.
 #include <cmath>
 

@@ -79,7 +79,7 @@ int fpdt_tw_experts_affine_fwd(const void* X, const void* W, const void* B, cons
         const Epilogue<ACT> behind = {static_cast<const uint16_t*>(B), static_cast<const uint16_t*>(R), static_cast<uint16_t*>(Z), static_cast<uint16_t*>(Y), join == FPDT_TW_JOIN_TIMES,
                                       all_wide(n_out, {B, R, Z, Y})};
         // (rows that are few for each expert, or weights that are few: us, 8 experts of 4096 x 14336 with a gate, 8 rows 111, tiles 136, 16 rows 152 and 164, 32 rows
-        // 164-173 and 159-188, card by card, 64 rows 201 and 196; 64 of 2048 x 1536, 64 rows 53 and 70; 8 of 1024 x 2048, 16 rows 9 and 12)
+        // 164-183 and 159-188, card by card, 64 rows 201 and 196; 64 of 2048 x 1536, 64 rows 53 and 70; 8 of 1024 x 2048, 16 rows 9 and 12)
         if (rows <= FEW_ROWS && (rows <= 4 * experts || few_pays(16, (int64_t)experts * n_in * n_out))) {
             experts_few_kernel<ACT><<<dim3((unsigned)((n_out + FEW_COLS - 1) / FEW_COLS), (unsigned)experts), FEW_WAVES * 64, 0, st>>>(
                 static_cast<const uint16_t*>(X), static_cast<const uint16_t*>(W), n_in, n_out, g, behind);
