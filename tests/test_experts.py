@@ -630,3 +630,38 @@ def test_gpu_group_of_experts_between_rows_that_are_not_finite(counts, first, n_
         want = d @ w
         assert bool(((dX[at].double() - want).abs() <= (n_out + 2) * 2.0 ** -24 * (d.abs() @ w.abs()) + 2.0 ** -8 * want.abs()).all()), e
         assert bool(((dW[e].double() - d.t() @ x).abs() <= (counts[e] + 2) * 2.0 ** -24 * (d.abs().t() @ x.abs())).all()), e
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,top,experts", [(2 ** 31 - 1, 1, 3), ((1 << 28) + 3, 7, 1000)])
+def test_gpu_sort_of_as_many_assignments_as_there_may_be(rows, top, experts):
+    """Places of every piece of the assignments continue those of the pieces before it."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    g = torch.Generator(device="cuda").manual_seed(top)
+    piece = torch.randint(-1, experts, ((1 << 24) + 11,), device="cuda", generator=g, dtype=torch.int32)
+    n = rows * top
+    expert = torch.empty(n, dtype=torch.int32, device="cuda")
+    for a in range(0, n, len(piece)):
+        expert[a:a + len(piece)] = piece[:min(len(piece), n - a)]
+    print("[case] sort", rows, top, experts, flush=True)
+    offsets, place = sort(expert.view(rows, top), experts)
+    place = place.view(-1)
+    # within a piece: what comes before in the order of experts, then as they come
+    def ranks(some):
+        order = torch.where(some < 0, experts, some).sort(stable=True).indices
+        counts = torch.bincount((some + 1).long(), minlength=experts + 1)[1:]
+        starts = torch.cat([counts.new_zeros(1), counts.cumsum(0)])
+        rank = torch.empty(len(some), dtype=torch.int64, device="cuda")
+        rank[order] = torch.arange(len(some), device="cuda")
+        return rank - starts[some.clamp(min=0).long()], counts
+    rank, counts = ranks(piece)
+    last, rest = ranks(piece[:n % len(piece)])
+    total = counts * (n // len(piece)) + rest
+    want = torch.cat([total.new_zeros(1), total.cumsum(0)])
+    assert torch.equal(offsets.long(), want)
+    before = want[:-1].clone()
+    for a in range(0, n, len(piece)):
+        some, r = (piece, rank) if a + len(piece) <= n else (piece[:n - a], last)
+        assert torch.equal(place[a:a + len(some)].long(), torch.where(some < 0, -1, before[some.clamp(min=0).long()] + r)), a
+        before += counts
