@@ -503,26 +503,26 @@ __global__ __launch_bounds__(256) void merge_kernel(const T* Oa, const float* La
                                                     const float* Lb, T* Oo, float* Lo, int64_t rows,
                                                     int Hq, int D)
 {
-    const int64_t pair = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     const int sub = threadIdx.x & 15;
-    if (pair >= rows * Hq) return;
-    const int64_t row = pair / Hq;
-    const int h = (int)(pair % Hq);
-    const float la = La[(size_t)h * rows + row], lb = Lb[(size_t)h * rows + row];
-    const float mx = fmaxf(la, lb);
-    float lse = -INFINITY, wa = 0.f, wb = 0.f;
-    if (mx > -INFINITY) {
-        lse = mx + logf(expf(la - mx) + expf(lb - mx));
-        wa = expf(la - lse);
-        wb = expf(lb - lse);
+    for (int64_t pair = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); pair < rows * Hq; pair += (int64_t)gridDim.x * 16) {
+        const int64_t row = pair / Hq;
+        const int h = (int)(pair % Hq);
+        const float la = La[(size_t)h * rows + row], lb = Lb[(size_t)h * rows + row];
+        const float mx = fmaxf(la, lb);
+        float lse = -INFINITY, wa = 0.f, wb = 0.f;
+        if (mx > -INFINITY) {
+            lse = mx + logf(expf(la - mx) + expf(lb - mx));
+            wa = expf(la - lse);
+            wb = expf(lb - lse);
+        }
+        for (int d = sub; d < D; d += 16) {
+            const size_t o = (size_t)pair * D + d;
+            const float xa = wa > 0.f ? load_elem(Oa + o) : 0.f;
+            const float xb = wb > 0.f ? load_elem(Ob + o) : 0.f;
+            store_elem(Oo + o, wa * xa + wb * xb);
+        }
+        if (sub == 0) Lo[(size_t)h * rows + row] = lse;
     }
-    for (int d = sub; d < D; d += 16) {
-        const size_t o = (size_t)pair * D + d;
-        const float xa = wa > 0.f ? load_elem(Oa + o) : 0.f;
-        const float xb = wb > 0.f ? load_elem(Ob + o) : 0.f;
-        store_elem(Oo + o, wa * xa + wb * xb);
-    }
-    if (sub == 0) Lo[(size_t)h * rows + row] = lse;
 }
 
 __global__ __launch_bounds__(256) void fill_kernel(uint4* p, size_t n16, unsigned char* tail, int ntail, unsigned word)
@@ -563,8 +563,7 @@ size_t f32_bwd_part_bytes(int64_t S, int Hq, int Hkv, int D) { return (size_t)f3
 void launch_merge(const void* Oa, const float* La, const void* Ob, const float* Lb, void* Oo,
                   float* Lo, int64_t rows, int Hq, int D, int is_bf16, hipStream_t st)
 {
-    const int64_t pairs = rows * Hq;
-    dim3 grid((unsigned)((pairs + 15) / 16));
+    const dim3 grid((unsigned)head_row_groups(rows * Hq));
     if (is_bf16)
         merge_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)Oa, La, (const uint16_t*)Ob, Lb,
                                                      (uint16_t*)Oo, Lo, rows, Hq, D);

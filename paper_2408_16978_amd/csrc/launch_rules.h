@@ -120,6 +120,10 @@ static inline int64_t bwd_prepare_blocks(int64_t S, int Hq, int Hkv) { return S 
 static const int64_t BWD_PREPARE_MOST = ((int64_t)1 << 23) - 1;
 static inline int64_t bwd_prepare_next(int64_t first, int64_t blocks) { return std::min(blocks - first, BWD_PREPARE_MOST); }
 
+// Workgroups of 256 lanes that take rows of heads 16 at a time, and walk those that are left: fewer than 2^32 lanes (of a launch of more the runtime
+// runs the remainder, without an error).
+static inline int64_t head_row_groups(int64_t pairs) { return std::min((pairs + 15) / 16, ((int64_t)1 << 24) - 1); }
+
 // Into how many splits a dK/dV launch divides the query walk of its key tiles.  Unsplit it has n_k / 256
 // * Hkv workgroups of four waves, one per compute unit: 64 at 8K tokens and two KV heads, so that three
 // quarters of the chip idle, and below the diagonal's last rows the longest workgroup decides.  Each

@@ -566,6 +566,7 @@ def test_more_tiles_than_a_launch_has_are_refused():
 @pytest.mark.parametrize("counts", [(2 ** 31 - 1,), (2 ** 30, 0, 5, 2 ** 29 + 77, 2 ** 28, 2 ** 27 - 100)])
 def test_gpu_products_of_as_many_rows_as_there_may_be(counts):
     """Narrow rows, 2^31 - 1 of them: tiles of 256 rows where those of 128 would be more than a launch has.  Small whole numbers, so that the products are exact."""
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 120 << 30:
         pytest.skip("needs 120 GB")
     rows, E, n = 2 ** 31 - 1, len(counts), 8
@@ -636,6 +637,7 @@ def test_gpu_group_of_experts_between_rows_that_are_not_finite(counts, first, n_
 @pytest.mark.parametrize("rows,top,experts", [(2 ** 31 - 1, 1, 3), ((1 << 28) + 3, 7, 1000)])
 def test_gpu_sort_of_as_many_assignments_as_there_may_be(rows, top, experts):
     """Places of every piece of the assignments continue those of the pieces before it."""
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 40 << 30:
         pytest.skip("needs 40 GB")
     g = torch.Generator(device="cuda").manual_seed(top)
