@@ -1054,14 +1054,14 @@ __global__ __launch_bounds__(256) void delta_kernel(const T* __restrict__ O, con
         for (int i = threadIdx.x; i < n_clear; i += 256) clear[i] = 0;
     // 16 lanes per (row, head): 4 pairs per wave, 16 pairs per workgroup
     const int tid = threadIdx.x;
-    const int64_t pair = (int64_t)blockIdx.x * 16 + (tid >> 4);
     const int sub = tid & 15;
-    if (pair >= rows * Hq) return;  // whole 16-lane groups leave together
-    const float acc = delta_of_row<T>(O + (size_t)pair * D, dO + (size_t)pair * D, D, sub);
-    if (sub == 0) {
-        const int64_t row = pair / Hq;
-        const int h = (int)(pair % Hq);
-        Delta[(size_t)h * stride + row] = acc;
+    for (int64_t pair = (int64_t)blockIdx.x * 16 + (tid >> 4); pair < rows * Hq; pair += (int64_t)gridDim.x * 16) {  // whole 16-lane groups leave together
+        const float acc = delta_of_row<T>(O + (size_t)pair * D, dO + (size_t)pair * D, D, sub);
+        if (sub == 0) {
+            const int64_t row = pair / Hq;
+            const int h = (int)(pair % Hq);
+            Delta[(size_t)h * stride + row] = acc;
+        }
     }
 }
 
@@ -1266,8 +1266,7 @@ void launch_stat_pack(const float* LSE, const float* Delta, int64_t stride, int6
 void launch_delta(const void* O, const void* dO, int64_t rows, int Hq, int D, int is_bf16,
                   float* Delta, int64_t delta_stride, hipStream_t st, unsigned* clear, int n_clear)
 {
-    const int64_t pairs = rows * Hq;
-    dim3 grid((unsigned)((pairs + 15) / 16));
+    const dim3 grid((unsigned)head_row_groups(rows * Hq));
     if (is_bf16)
         delta_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)O, (const uint16_t*)dO, rows, Hq, D, Delta, delta_stride, clear, n_clear);
     else

@@ -32,3 +32,31 @@ def test_gpu_merge():
         o, l = torch.empty_like(Oa[at]), torch.empty_like(la)
         B.fpdt_attn_merge(Oa[at], la, Ob[at], lb, o, l)
         assert torch.equal(O[at], o) and torch.equal(L[:, at], l), r
+
+
+@pytest.mark.gpu
+def test_gpu_backward_pair_by_pair():
+    """65600 query heads of 4096 tokens, 2^28 rows of heads and a few: 64 heads, each of them 1025 times in its group, so that every repetition's dQ has the bits of the first, and that the value
+    that the 64 heads alone give (the tolerance of the bf16 gradients)."""
+    _room(215)
+    S, few, times, D = 4096, 64, 1025, 64
+    scale = D ** -0.5
+    small = runner.make_buffers(*inputs.make_qkvdo(S, few, few, D, "bf16", 52, device="cuda"), 256, scale, B.FPDT_PAIRWISE)
+    runner.forward(small)
+    runner.backward(small)
+    torch.cuda.synchronize()
+    wide = lambda t: t.repeat_interleave(times, 1)
+    Q, dO, O = wide(small.Q), wide(small.dO), wide(small.O)
+    LSE = small.LSE.repeat_interleave(times, 0)
+    dQ, dK, dV = torch.full_like(Q, float("nan")), torch.empty_like(small.K), torch.empty_like(small.V)
+    ws = B.alloc_workspace(S, 256, few * times, few, D, B.FPDT_DTYPE_BF16, B.FPDT_PAIRWISE, True)
+    ws.fill_(255)
+    print("[case] backward pair by pair", S, few * times, D, flush=True)
+    B.fpdt_attn_bwd(Q, small.K, small.V, O, LSE, dO, dQ, dK, dV, 256, scale, B.FPDT_PAIRWISE, ws)
+    torch.cuda.synchronize()
+    got = dQ.view(S, few, times, D)
+    for r in range(0, S, 256):
+        assert torch.equal(got[r:r + 256], got[r:r + 256, :, :1].expand(-1, -1, times, -1)), r
+    want = small.dQ.double()
+    rms = want.pow(2).mean().sqrt()
+    assert float((got[:, :, 0].double() - want).abs().max() / rms) <= 2e-2 * max(1.0, float(want.abs().max() / rms))
