@@ -216,13 +216,18 @@ __global__ __launch_bounds__(NT) void loss_rows_kernel(const float* __restrict__
 // with gradients: 8192 logits 133 | 150, 12288 184 | 192, 16380 254 | 259).  Without gradients there is no second
 // pass: nothing is kept, and two rows fit a compute unit (forward, 4096 rows of 18432 logits 133 -> 114 us, 1058 of 32000
 // 62 -> 57.5; with one row at a time 16384 to 20000 logits took up to 8% longer than with 256 threads).  The bits are the same.
-constexpr int LOSS_WIDE = 16384;
+// LOSS_MOST rows a launch: fewer than 2^32 threads of either width.
+constexpr int LOSS_WIDE = 16384, LOSS_MOST = 1 << 21;
 void launch_loss_rows(const float* logits, int64_t ldl, const int32_t* target, int rows, int vocab, float grad_scale, float* loss, float* lse, uint16_t* G, int64_t ldg, hipStream_t st)
 {
-    const dim3 grid((unsigned)rows);
-    if (vocab >= LOSS_WIDE && G) loss_rows_kernel<1024, 32768><<<grid, 1024, 0, st>>>(logits, ldl, target, vocab, grad_scale, loss, lse, G, ldg);
-    else if (vocab >= LOSS_WIDE) loss_rows_kernel<1024, 0><<<grid, 1024, 0, st>>>(logits, ldl, target, vocab, grad_scale, loss, lse, G, ldg);
-    else loss_rows_kernel<256, 0><<<grid, 256, 0, st>>>(logits, ldl, target, vocab, grad_scale, loss, lse, G, ldg);
+    for (int r = 0; r < rows; r += LOSS_MOST) {
+        const dim3 grid((unsigned)(rows - r < LOSS_MOST ? rows - r : LOSS_MOST));
+        const float* x = logits + (size_t)r * ldl;
+        uint16_t* g = G ? G + (size_t)r * ldg : nullptr;
+        if (vocab >= LOSS_WIDE && G) loss_rows_kernel<1024, 32768><<<grid, 1024, 0, st>>>(x, ldl, target + r, vocab, grad_scale, loss + r, lse + r, g, ldg);
+        else if (vocab >= LOSS_WIDE) loss_rows_kernel<1024, 0><<<grid, 1024, 0, st>>>(x, ldl, target + r, vocab, grad_scale, loss + r, lse + r, g, ldg);
+        else loss_rows_kernel<256, 0><<<grid, 256, 0, st>>>(x, ldl, target + r, vocab, grad_scale, loss + r, lse + r, g, ldg);
+    }
 }
 
 // ---- feed-forward elementwise kernels (bf16 in / out, fp32 arithmetic) ----

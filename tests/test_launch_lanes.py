@@ -60,3 +60,29 @@ def test_gpu_backward_pair_by_pair():
     want = small.dQ.double()
     rms = want.pow(2).mean().sqrt()
     assert float((got[:, :, 0].double() - want).abs().max() / rms) <= 2e-2 * max(1.0, float(want.abs().max() / rms))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grads", [False, True])
+def test_gpu_loss_of_the_longest_chunk(grads):
+    """2^24 rows in one chunk, of eight logits, which repeat: every repetition has the bits of the first, and that those of a call of its own."""
+    _room(20)
+    rows, hidden, vocab, period = 1 << 24, 8, 8, 1 << 14
+    g = torch.Generator(device="cuda").manual_seed(2)
+    few = torch.randn(period, hidden, device="cuda", generator=g).to(torch.bfloat16)
+    W = torch.randn(vocab, hidden, device="cuda", generator=g).to(torch.bfloat16)
+    some = torch.randint(0, vocab, (period,), device="cuda", generator=g, dtype=torch.int32)
+
+    def run(H, target):
+        n = len(H)
+        ws = torch.empty(TW.fpdt_tw_loss_workspace_bytes(n, hidden, vocab, 1), dtype=torch.uint8, device="cuda")
+        ws.fill_(255)
+        loss, lse = (torch.full((n,), float("nan"), device="cuda") for _ in range(2))
+        dH = torch.full_like(H, float("nan")) if grads else None
+        TW.fpdt_tw_loss_fwd_bwd(H, W, target, 2.0 ** -14, loss, lse, dH, None, 1, ws)
+        torch.cuda.synchronize()
+        return loss, lse, dH
+
+    print("[case] loss of 2^24 rows", grads, flush=True)
+    for got, want in zip(run(few.repeat(rows // period, 1), some.repeat(rows // period)), run(few, some)):
+        assert want is None or (bool(torch.isfinite(want).all()) and torch.equal(got.view(-1, *want.shape), want.expand(rows // period, *want.shape)))
